@@ -291,6 +291,96 @@ int exfold_moe_decode_layer(const exfold_layer *layer, const void *x, const void
                             const exfold_decode_meta *meta, void *ws, size_t ws_bytes, void *cuda_stream);
 
 /*
+ * Routing by a model's own router (Eq. 2 is the softmax router with renormalised weights; many models rank otherwise).
+ * With z the router scores of a token and N experts in n_groups groups of consecutive experts:
+ *     s_e = softmax(z)_e or sigmoid(z_e)
+ *     c_e = s_e + bias_e          the bias (load balance) takes part in the choice only
+ *     groups: the top_groups groups of the largest group score stay, the others' experts are no candidates; a group's
+ *             score is its largest c, or the sum of its two largest
+ *     ids   = the K candidates of the largest c, descending; ties, also between groups, go to the lower index
+ *     w_k   = scale * s_k, or scale * s_k / sum_j s_j over the chosen (0 where that sum is 0)
+ * c is compared as computed in 64 bits (without a bias and with the groups' largest c: as z itself, the same order).
+ * A score of -infinity or of the lowest finite value masks its expert: chosen behind every unmasked candidate, s = 0,
+ * left out of the softmax and of the sum of two; a token whose experts are all masked gets weights 0. A NaN score ranks
+ * first and makes its token's weights NaN where they depend on it. ids are always K different experts.
+ */
+enum { EXFOLD_SCORE_SOFTMAX = 0, EXFOLD_SCORE_SIGMOID = 1 };
+enum { EXFOLD_GROUP_MAX = 0, EXFOLD_GROUP_TOP2 = 1 };
+typedef struct {
+    int32_t score;       /* EXFOLD_SCORE_* */
+    int32_t n_groups;    /* 1..32, a divisor of N */
+    int32_t top_groups;  /* 1..n_groups; top_groups * N / n_groups >= K */
+    int32_t group_score; /* EXFOLD_GROUP_* */
+    int32_t renormalise; /* != 0: the chosen scores are divided by their sum */
+    float scale;         /* finite */
+    const float *bias;   /* [N] (device) or NULL */
+} exfold_router;
+
+/*
+ * logits [T][N] fp32 -> ids [T][K] int32, w [T][K] fp32 and, if not NULL, load [N] int32: how many tokens chose each
+ * expert (overwritten). `layer` gives N and K. T in [0, 2^24] (T = 0: load is cleared). No workspace: one kernel, and
+ * for more than one block of tokens and a load a clearing of `load` before it. ids and w are the arguments of
+ * exfold_moe_prefill_routed / exfold_moe_decode_routed.
+ */
+int exfold_route(const exfold_layer *layer, const float *logits, int64_t T, const exfold_router *router, int32_t *ids,
+                 float *w, int32_t *load, void *cuda_stream);
+
+/*
+ * Gradient of exfold_route's weights for tuning a router: dw [T][K] = dLoss/dw -> dlogits [T][N] = dLoss/dlogits, every
+ * element written. The choice is a constant, so the bias and the groups play no part (`router` gives score, renormalise
+ * and scale). ids as exfold_route wrote them; an id outside [0, N) has no gradient. With g = dw, p_k = s_k / sum_j s_j and
+ * gm = sum_j g_j p_j over the chosen:
+ *     renormalised      softmax scale p_k (g_k - gm), sigmoid the same times (1 - s_k); 0 for the other experts
+ *     not renormalised  sigmoid scale g_k s_k (1 - s_k), 0 for the others; softmax scale s_e ([e chosen] g_e - sum_k g_k s_k)
+ * Masked experts get 0, and so does a token whose chosen scores sum to 0.
+ */
+int exfold_route_backward(const exfold_layer *layer, const float *logits, const int32_t *ids, const float *dw, int64_t T,
+                          const exfold_router *router, float *dlogits, void *cuda_stream);
+
+/*
+ * The folded layer on given routes, for routers that Eq. 2 does not describe: exfold_moe_prefill_ex and
+ * exfold_moe_decode with ids [T][K] int32 and w [T][K] fp32 (device) in the place of the logits, everything else alike.
+ * A token's K experts are different ones, in any order. An id outside [0, N) counts as expert 0 with weight 0.
+ * Prefill (Eq. 10): routes are ranked by w h (one fp32 product; ties -> lower id) and keep their given weights; opts as in
+ * exfold_moe_prefill_ex. With k_pre = K `tables` may be NULL (nothing is folded; slots are ranked by w).
+ * Decode (Eq. 11): pool scores are h_e times the sum of the given weights, which are at least 0 and below 8.
+ */
+int exfold_moe_prefill_routed(const exfold_layer *layer, const void *x, const int32_t *ids, const float *w, int64_t T,
+                              const void *w_gate, const void *w_up, const void *w_down, const exfold_tables *tables,
+                              int32_t k_pre, const exfold_fold_opts *opts, void *y, const exfold_prefill_meta *meta,
+                              void *ws, size_t ws_bytes, void *cuda_stream);
+int exfold_moe_decode_routed(const exfold_layer *layer, const void *x, const int32_t *ids, const float *w, int64_t B,
+                             const void *w_gate, const void *w_up, const void *w_down, const exfold_tables *tables,
+                             int32_t pool_m, void *y, const exfold_decode_meta *meta, void *ws, size_t ws_bytes,
+                             void *cuda_stream);
+
+/*
+ * A dense product with its epilogue: the projections before and after the layer (to and from the residual stream, dense
+ * FFN layers).
+ *     y[i][o] = act( sum_k x[i][k] w[o][k] + bias[o] ) + residual[i][o]
+ * x [T][in], w [out][in] (nn.Linear) and bias [out] in `dtype`, y and residual [T][out] in `out_dtype` (fp32 for fp32
+ * inputs; fp32 or bf16 for bf16). Sums, epilogue and activation in fp32, one rounding at the end. bias and residual may be
+ * NULL. The ld fields are the distances between rows in elements (0: dense). residual may be y itself (the same rows and
+ * distance); y overlaps no other operand.
+ * Any sizes from 1 (in, out <= 2^24, T in [0, 2^24], T = 0 writes nothing). bf16 operands on the tensor cores need x and w
+ * 16-byte aligned and ldx, ldw multiples of 8 elements; others, and fp32, run on a CUDA-core kernel.
+ * Results do not depend on other calls: no atomics, sums in a fixed order for the given sizes.
+ * Workspace: exfold_linear_workspace_bytes (256-byte aligned; its first 256 bytes are the status record of
+ * exfold_device_status). Calls that share a workspace must be ordered on one stream.
+ */
+enum { EXFOLD_ACT_NONE = 0, EXFOLD_ACT_RELU = 1, EXFOLD_ACT_GELU = 2, EXFOLD_ACT_GELU_TANH = 3, EXFOLD_ACT_SILU = 4 };
+typedef struct {
+    int64_t in_features, out_features;
+    int32_t dtype;      /* exfold_dtype of x, w, bias */
+    int32_t out_dtype;  /* exfold_dtype of y, residual */
+    int32_t activation; /* EXFOLD_ACT_* (GELU: with the error function; GELU_TANH: its tanh form) */
+    int64_t ldx, ldw, ldy, ldr;
+} exfold_linear_desc;
+size_t exfold_linear_workspace_bytes(const exfold_linear_desc *desc, int64_t max_tokens);
+int exfold_linear(const exfold_linear_desc *desc, const void *x, const void *w, const void *bias, const void *residual,
+                  int64_t T, void *y, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/*
  * The same two calls for activations that live in HOST memory (pinned for real overlap):
  * x_host, logits_host and y_host are host pointers; the call stages them through the
  * workspace with asynchronous copies on the stream (x and logits in before the layer, y out

@@ -25,13 +25,18 @@ EXFOLD_ERR_DEVICE_TIMEOUT = -5
 EXFOLD_ERR_EXCEEDS_STATIC_SCRATCH = -6
 EXFOLD_STATIC_SCRATCH_BYTES = 8 << 20
 EXFOLD_WARN_UNOBSERVED_EXPERT = 1
+SCORES = {"softmax": 0, "sigmoid": 1}
+GROUP_SCORES = {"max": 0, "top2": 1}
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
 EXPORTS = ["exfold_workspace_bytes", "exfold_host_staging_bytes", "exfold_calibrate", "exfold_moe_prefill",
            "exfold_moe_decode", "exfold_moe_prefill_host", "exfold_moe_decode_host", "exfold_device_status",
            "exfold_status_string", "exfold_launch_count", "exfold_profile_enable", "exfold_profile_read",
            "exfold_moe_decode_noalloc", "exfold_static_pool_build", "exfold_moe_decode_static",
            "exfold_moe_prefill_ex", "exfold_router_logits", "exfold_calibrate_layers", "exfold_device_status_noalloc",
-           "exfold_static_scratch_address", "exfold_thread_release", "exfold_moe_prefill_layer", "exfold_moe_decode_layer"]
+           "exfold_static_scratch_address", "exfold_thread_release", "exfold_moe_prefill_layer", "exfold_moe_decode_layer",
+           "exfold_route", "exfold_route_backward", "exfold_moe_prefill_routed", "exfold_moe_decode_routed",
+           "exfold_linear_workspace_bytes", "exfold_linear"]
 PROFILE_SLOTS = ["prefill_route", "prefill_scan", "prefill_scatter", "gemm1_gateup_swiglu", "gemm2_down_combine",
                  "convert_bf16", "decode_route", "decode_gather", "decode_gateup", "decode_down", "ffn_f32",
                  "combine_f32", "gemm1_pair_pass", "gemm2_pair_pass", "decode_ffn"]
@@ -73,6 +78,16 @@ class exfold_fold_opts(C.Structure):
 
 class exfold_static_pool(C.Structure):
     _fields_ = [("pool_ids", C.c_void_p), ("target", C.c_void_p), ("scale", C.c_void_p), ("pool_m", C.c_int32)]
+
+
+class exfold_router(C.Structure):
+    _fields_ = [("score", C.c_int32), ("n_groups", C.c_int32), ("top_groups", C.c_int32), ("group_score", C.c_int32),
+                ("renormalise", C.c_int32), ("scale", C.c_float), ("bias", C.c_void_p)]
+
+
+class exfold_linear_desc(C.Structure):
+    _fields_ = [("in_features", C.c_int64), ("out_features", C.c_int64), ("dtype", C.c_int32), ("out_dtype", C.c_int32),
+                ("activation", C.c_int32), ("ldx", C.c_int64), ("ldw", C.c_int64), ("ldy", C.c_int64), ("ldr", C.c_int64)]
 
 
 def _load() -> C.CDLL:
@@ -119,6 +134,20 @@ def _load() -> C.CDLL:
     lib.exfold_moe_decode_static.restype = C.c_int
     lib.exfold_moe_decode_static.argtypes = [C.POINTER(exfold_layer), vp, vp, i64, vp, vp, vp,
                                              C.POINTER(exfold_static_pool), vp, C.POINTER(exfold_decode_meta), vp, sz, vp]
+    lib.exfold_route.restype = C.c_int
+    lib.exfold_route.argtypes = [C.POINTER(exfold_layer), vp, i64, C.POINTER(exfold_router), vp, vp, vp, vp]
+    lib.exfold_route_backward.restype = C.c_int
+    lib.exfold_route_backward.argtypes = [C.POINTER(exfold_layer), vp, vp, vp, i64, C.POINTER(exfold_router), vp, vp]
+    lib.exfold_moe_prefill_routed.restype = C.c_int
+    lib.exfold_moe_prefill_routed.argtypes = [C.POINTER(exfold_layer), vp, vp, vp, i64, vp, vp, vp, C.POINTER(exfold_tables), i32,
+                                              C.POINTER(exfold_fold_opts), vp, C.POINTER(exfold_prefill_meta), vp, sz, vp]
+    lib.exfold_moe_decode_routed.restype = C.c_int
+    lib.exfold_moe_decode_routed.argtypes = [C.POINTER(exfold_layer), vp, vp, vp, i64, vp, vp, vp, C.POINTER(exfold_tables), i32,
+                                             vp, C.POINTER(exfold_decode_meta), vp, sz, vp]
+    lib.exfold_linear_workspace_bytes.restype = sz
+    lib.exfold_linear_workspace_bytes.argtypes = [C.POINTER(exfold_linear_desc), i64]
+    lib.exfold_linear.restype = C.c_int
+    lib.exfold_linear.argtypes = [C.POINTER(exfold_linear_desc), vp, vp, vp, vp, i64, vp, vp, sz, vp]
     lib.exfold_device_status.restype = C.c_int
     lib.exfold_device_status.argtypes = [vp, vp]
     lib.exfold_device_status_noalloc.restype = C.c_int
@@ -382,4 +411,111 @@ def exfold_moe_prefill_ex(layer, x, logits, w_gate, w_up, w_down, tables: exfold
                                    _ptr(ws), ws.numel(), _stream(stream))
     if check and rc != 0:
         raise ExfoldError(rc, "exfold_moe_prefill_ex")
+    return rc
+
+
+def make_router(score: str = "softmax", bias: Optional[torch.Tensor] = None, n_groups: int = 1, top_groups: int = 1,
+                group_score: str = "max", renormalise: bool = True, scale: float = 1.0) -> exfold_router:
+    """A model's own router (exfold_route). `bias`: fp32 [N] on the device, kept alive by the returned struct."""
+    assert bias is None or bias.dtype == torch.float32
+    r = exfold_router(SCORES[score], n_groups, top_groups, GROUP_SCORES[group_score], int(renormalise), scale, _ptr(bias))
+    r.bias_tensor = bias
+    return r
+
+
+def _typed(t: Optional[torch.Tensor], dtype, shape) -> Optional[int]:
+    if t is not None:
+        assert t.dtype == dtype and tuple(t.shape) == tuple(shape), f"expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}"
+    return _ptr(t)
+
+
+def exfold_route(layer, logits, router: exfold_router, ids, w, load=None, stream=None, check: bool = True) -> int:
+    """logits [T][N] fp32 -> ids [T][K] int32, w [T][K] fp32, load [N] int32 (tokens per expert)."""
+    T, N, K = logits.shape[0], layer.n_experts, layer.top_k
+    rc = lib.exfold_route(C.byref(layer), _typed(logits, torch.float32, (T, N)), T, C.byref(router),
+                          _typed(ids, torch.int32, (T, K)), _typed(w, torch.float32, (T, K)),
+                          _typed(load, torch.int32, (N,)), _stream(stream))
+    if check and rc != 0:
+        raise ExfoldError(rc, "exfold_route")
+    return rc
+
+
+def exfold_route_backward(layer, logits, ids, dw, router: exfold_router, dlogits, stream=None, check: bool = True) -> int:
+    """dw [T][K], the gradient of exfold_route's weights -> dlogits [T][N]."""
+    T, N, K = logits.shape[0], layer.n_experts, layer.top_k
+    rc = lib.exfold_route_backward(C.byref(layer), _typed(logits, torch.float32, (T, N)), _typed(ids, torch.int32, (T, K)),
+                                   _typed(dw, torch.float32, (T, K)), T, C.byref(router),
+                                   _typed(dlogits, torch.float32, (T, N)), _stream(stream))
+    if check and rc != 0:
+        raise ExfoldError(rc, "exfold_route_backward")
+    return rc
+
+
+def exfold_moe_prefill_routed(layer, x, ids, w, w_gate, w_up, w_down, tables: Optional[exfold_tables], k_pre: int, y, ws,
+                              loss_threshold: float = float("inf"), rescale: bool = False, confidence_split: bool = False,
+                              gemm_path: int = 0, meta: Optional[dict] = None, stream=None, check: bool = True) -> int:
+    """exfold_moe_prefill_ex on given routes ids, w [T][K]. tables may be None where k_pre = K."""
+    T, K = x.shape[0], layer.top_k
+    opts = exfold_fold_opts(loss_threshold, int(rescale), int(confidence_split), int(gemm_path))
+    rc = lib.exfold_moe_prefill_routed(C.byref(layer), _ptr(x), _typed(ids, torch.int32, (T, K)),
+                                       _typed(w, torch.float32, (T, K)), T, _ptr(w_gate), _ptr(w_up), _ptr(w_down),
+                                       C.byref(tables) if tables is not None else None, k_pre, C.byref(opts), _ptr(y),
+                                       _prefill_meta(meta), _ptr(ws), ws.numel(), _stream(stream))
+    if check and rc != 0:
+        raise ExfoldError(rc, "exfold_moe_prefill_routed")
+    return rc
+
+
+def exfold_moe_decode_routed(layer, x, ids, w, w_gate, w_up, w_down, tables: exfold_tables, pool_m: int, y, ws,
+                             meta: Optional[dict] = None, stream=None, check: bool = True) -> int:
+    """exfold_moe_decode on given routes ids, w [B][K]."""
+    B, K = x.shape[0], layer.top_k
+    rc = lib.exfold_moe_decode_routed(C.byref(layer), _ptr(x), _typed(ids, torch.int32, (B, K)),
+                                      _typed(w, torch.float32, (B, K)), B, _ptr(w_gate), _ptr(w_up), _ptr(w_down),
+                                      C.byref(tables), pool_m, _ptr(y), _decode_meta(meta), _ptr(ws), ws.numel(),
+                                      _stream(stream))
+    if check and rc != 0:
+        raise ExfoldError(rc, "exfold_moe_decode_routed")
+    return rc
+
+
+_LINEAR_DTYPES = {torch.float32: EXFOLD_F32, torch.bfloat16: EXFOLD_BF16}
+
+
+def _rows(t: Optional[torch.Tensor], dtype, shape):
+    """Pointer and row distance of a matrix whose rows are contiguous."""
+    if t is None:
+        return None, 0
+    assert t.dtype == dtype and tuple(t.shape) == tuple(shape), f"expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}"
+    assert t.stride(1) == 1 or t.shape[1] == 1, "rows must be contiguous"
+    assert t.stride(0) >= t.shape[1] or t.shape[0] <= 1, "rows must not overlap"
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else 0)
+
+
+def exfold_linear_workspace_bytes(desc: exfold_linear_desc, max_tokens: int) -> int:
+    return int(lib.exfold_linear_workspace_bytes(C.byref(desc), max_tokens))
+
+
+def alloc_linear_workspace(in_features: int, out_features: int, max_tokens: int, dtype, out_dtype=None,
+                           device="cuda") -> torch.Tensor:
+    """Workspace of exfold_linear for products of this shape with up to max_tokens rows and any row distances."""
+    desc = exfold_linear_desc(in_features, out_features, _LINEAR_DTYPES[dtype], _LINEAR_DTYPES[out_dtype or dtype], 0, 0, 0, 0, 0)
+    n = exfold_linear_workspace_bytes(desc, max_tokens)
+    if n == 0:
+        raise ExfoldError(EXFOLD_ERR_INVALID_ARG, "exfold_linear_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def exfold_linear(x, w, y, ws, bias=None, residual=None, activation: str = "none", stream=None, check: bool = True) -> int:
+    """y = act(x w^T + bias) + residual. x [T][in], w [out][in], bias [out] of one type; y, residual [T][out]. The matrices may
+    have any distance between their rows."""
+    T, i, o = x.shape[0], x.shape[1], w.shape[0]
+    xp, ldx = _rows(x, x.dtype, (T, i))
+    wp, ldw = _rows(w, x.dtype, (o, i))
+    yp, ldy = _rows(y, y.dtype, (T, o))
+    rp, ldr = _rows(residual, y.dtype, (T, o))
+    desc = exfold_linear_desc(i, o, _LINEAR_DTYPES[x.dtype], _LINEAR_DTYPES[y.dtype], ACTIVATIONS[activation], ldx, ldw, ldy, ldr)
+    rc = lib.exfold_linear(C.byref(desc), xp, wp, _typed(bias, x.dtype, (o,)), rp, T, yp, _ptr(ws), ws.numel(), _stream(stream))
+    if check and rc != 0:
+        raise ExfoldError(rc, "exfold_linear")
     return rc

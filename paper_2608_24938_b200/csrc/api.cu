@@ -538,11 +538,17 @@ int exfold_moe_prefill(const exfold_layer* layer, const void* x, const float* lo
                                  ws_bytes, cuda_stream);
 }
 
-int exfold_moe_prefill_ex(const exfold_layer* layer, const void* x, const float* logits, int64_t T,
-                          const void* w_gate, const void* w_up, const void* w_down, const exfold_tables* tables,
-                          int32_t k_pre, const exfold_fold_opts* opts, void* y, const exfold_prefill_meta* meta,
-                          void* ws, size_t ws_bytes, void* cuda_stream) {
-    int rc = check_common(layer, x, logits, T, w_gate, w_up, w_down, tables, y, ws);
+// The routes of a call whose router is the caller's: [T][K] experts and weights in the place of the scores
+struct GivenRoutes {
+    const int32_t* ids;
+    const float* w;
+};
+
+static int prefill_impl(const exfold_layer* layer, const void* x, const float* logits, const GivenRoutes* given, int64_t T,
+                        const void* w_gate, const void* w_up, const void* w_down, const exfold_tables* tables, int32_t k_pre,
+                        const exfold_fold_opts* opts, void* y, const exfold_prefill_meta* meta, void* ws, size_t ws_bytes,
+                        void* cuda_stream) {
+    int rc = check_common(layer, x, given ? given->w : logits, T, w_gate, w_up, w_down, tables, y, ws);
     if (rc != EXFOLD_OK) return rc;
     const exfold_layer& l = *layer;
     if (k_pre < 1 || k_pre > l.top_k) return EXFOLD_ERR_INVALID_ARG;
@@ -593,10 +599,15 @@ int exfold_moe_prefill_ex(const exfold_layer* layer, const void* x, const float*
     rp.queue = mixed ? at<DeviceStatus>(ws, pl.status)->queue : nullptr;
     // few tokens of an fp32 layer: its FFN kernel routes them itself
     const int tile_rows = mixed ? kMixedTiles : bf16 ? kTileM : ffn_f32_tile_rows(Rtot, G, d, I, sm_count());
-    const bool routed = !bf16 && ffn_f32_routes(false, T, Rtot, G, N, Kp, d, I, tile_rows, sm_count());
+    const bool routed = !bf16 && !given && ffn_f32_routes(false, T, Rtot, G, N, Kp, d, I, tile_rows, sm_count());
     // (so do the small-batch kernels, unless the caller asks for the metadata, of which the scatter kernel writes a part)
-    const bool small_routed = small && meta == nullptr;
-    if (!routed && !small_routed) { ProfScope ps(0, s); EXFOLD_CUDA(launch_prefill_route(rp, s)); }
+    const bool small_routed = small && meta == nullptr && !given;
+    if (given) {
+        PrefillGivenParams gp{};
+        gp.r = rp; gp.in_ids = given->ids; gp.in_w = given->w; gp.h = tables->h;
+        ProfScope ps(0, s);
+        EXFOLD_CUDA(launch_prefill_given(gp, s));
+    } else if (!routed && !small_routed) { ProfScope ps(0, s); EXFOLD_CUDA(launch_prefill_route(rp, s)); }
 
     // The shared expert's gate/up projection needs nothing the routing kernels produce (its rows are x itself, its
     // rows of H lie behind the routed ones): its whole row-tile pairs run on the second stream beside the scatter
@@ -704,15 +715,40 @@ int exfold_moe_prefill_ex(const exfold_layer* layer, const void* x, const float*
     return EXFOLD_OK;
 }
 
+int exfold_moe_prefill_ex(const exfold_layer* layer, const void* x, const float* logits, int64_t T,
+                          const void* w_gate, const void* w_up, const void* w_down, const exfold_tables* tables,
+                          int32_t k_pre, const exfold_fold_opts* opts, void* y, const exfold_prefill_meta* meta,
+                          void* ws, size_t ws_bytes, void* cuda_stream) {
+    return prefill_impl(layer, x, logits, nullptr, T, w_gate, w_up, w_down, tables, k_pre, opts, y, meta, ws, ws_bytes, cuda_stream);
+}
+
+int exfold_moe_prefill_routed(const exfold_layer* layer, const void* x, const int32_t* ids, const float* w, int64_t T,
+                              const void* w_gate, const void* w_up, const void* w_down, const exfold_tables* tables,
+                              int32_t k_pre, const exfold_fold_opts* opts, void* y, const exfold_prefill_meta* meta,
+                              void* ws, size_t ws_bytes, void* cuda_stream) {
+    if (!ids || ((reinterpret_cast<uintptr_t>(ids) | reinterpret_cast<uintptr_t>(w)) & 3) != 0) return EXFOLD_ERR_INVALID_ARG;
+    exfold_tables none{};
+    if (tables == nullptr) {  // nothing is folded: no table is read (any pointer passes the check that they are there)
+        if (!layer || k_pre != layer->top_k) return EXFOLD_ERR_INVALID_ARG;
+        none.S = none.L = none.lnh = const_cast<float*>(w);
+        none.h = none.S;
+    }
+    const GivenRoutes given{ids, w};
+    return prefill_impl(layer, x, nullptr, &given, T, w_gate, w_up, w_down, tables ? tables : &none, k_pre, opts, y, meta, ws,
+                        ws_bytes, cuda_stream);
+}
+
 static int router_enqueue(const exfold_layer* layer, const void* x, const void* w_router, int64_t T, float* logits,
                           void* ws, size_t ws_bytes, cudaStream_t s, bool clear_status);
 
 // Dynamic (tables != null) or static (spool != null) decode step.
 // w_router != null: the router scores are computed first (into `logits`, which is then an output).
+// given != null: routes in the place of the scores.
 static int decode_impl(const exfold_layer* layer, const void* x, const float* logits, int64_t B, const void* w_gate,
                        const void* w_up, const void* w_down, const exfold_tables* tables,
                        const exfold_static_pool* spool, int32_t pool_m, void* y, const exfold_decode_meta* meta,
-                       void* ws, size_t ws_bytes, void* cuda_stream, const void* w_router = nullptr) {
+                       void* ws, size_t ws_bytes, void* cuda_stream, const void* w_router = nullptr,
+                       const GivenRoutes* given = nullptr) {
     exfold_tables dummy{};  // the static path needs no tables: satisfy the common pointer checks
     if (spool != nullptr) {
         if (!spool->pool_ids || !spool->target || !spool->scale) return EXFOLD_ERR_INVALID_ARG;
@@ -720,7 +756,7 @@ static int decode_impl(const exfold_layer* layer, const void* x, const float* lo
         tables = &dummy;
         pool_m = spool->pool_m;
     }
-    int rc = check_common(layer, x, logits, B, w_gate, w_up, w_down, tables, y, ws);
+    int rc = check_common(layer, x, given ? given->w : logits, B, w_gate, w_up, w_down, tables, y, ws);
     if (rc != EXFOLD_OK) return rc;
     const exfold_layer& l = *layer;
     if (pool_m < 1 || pool_m > l.n_experts) return EXFOLD_ERR_INVALID_ARG;
@@ -767,11 +803,12 @@ static int decode_impl(const exfold_layer* layer, const void* x, const float* lo
         // the remapped slots go to a second array: the Top-K ids are read by every CTA while one of them writes
         int32_t* const out_ids = at<int32_t>(ws, pl.perm);
         if (decode_small_fits((int)B, K, d, w_gate, w_up, w_down)) {
-            if (w_router != nullptr) { ProfScope ps(6, s); EXFOLD_CUDA(launch_decode_topk(tp, s)); }
+            const bool ranked = w_router != nullptr || given != nullptr;  // by a kernel before
+            if (ranked) { ProfScope ps(6, s); EXFOLD_CUDA(given ? launch_decode_given(tp, given->ids, given->w, s) : launch_decode_topk(tp, s)); }
             DecodeSmallParams sp{};
             sp.x = tp.x; sp.wg = reinterpret_cast<const __nv_bfloat16*>(w_gate); sp.wu = reinterpret_cast<const __nv_bfloat16*>(w_up);
             sp.wd = reinterpret_cast<const __nv_bfloat16*>(w_down); sp.y = reinterpret_cast<__nv_bfloat16*>(y);
-            sp.logits = w_router == nullptr ? logits : nullptr; sp.ids = tp.ids; sp.w64 = tp.w64;
+            sp.logits = ranked ? nullptr : logits; sp.ids = tp.ids; sp.w64 = tp.w64;
             sp.S = tables->S; sp.L = tables->L; sp.h = tables->h;
             sp.st_pool = rp.st_pool; sp.st_target = rp.st_target; sp.st_scale = rp.st_scale;
             sp.B = (int)B; sp.N = N; sp.K = K; sp.M = pool_m; sp.n_shared = l.n_shared; sp.d = d; sp.I = I;
@@ -782,7 +819,7 @@ static int decode_impl(const exfold_layer* layer, const void* x, const float* lo
             }
             sp.H = at<__nv_bfloat16>(ws, pl.H); sp.row_tok = rp.row_tok; sp.row_w = rp.row_w;
             sp.row_grp = at<int32_t>(ws, pl.row_grp); sp.grp_expert = rp.grp_expert; sp.n_groups = rp.n_groups;
-            sp.status = w_router == nullptr ? rp.status : nullptr;
+            sp.status = ranked ? nullptr : rp.status;
             { ProfScope ps(14, s); EXFOLD_CUDA(launch_decode_small(sp, nullptr, sm_count(), s)); }
         } else {
             // Token-parallel Top-K (with the router scores when w_router is given) -> gate/up kernel that finishes the
@@ -813,7 +850,7 @@ static int decode_impl(const exfold_layer* layer, const void* x, const float* lo
                 !make_tmap(&fp.tm_wg64, w_gate, E * I, d, 64) || !make_tmap(&fp.tm_wu64, w_up, E * I, d, 64) ||
                 (alt && (!make_tmap(&fp.tm_wg_alt, w_gate, E * I, d, alt) || !make_tmap(&fp.tm_wu_alt, w_up, E * I, d, alt))))
                 return EXFOLD_ERR_CUDA;
-            { ProfScope ps(6, s); EXFOLD_CUDA(launch_decode_topk(tp, s)); }
+            { ProfScope ps(6, s); EXFOLD_CUDA(given ? launch_decode_given(tp, given->ids, given->w, s) : launch_decode_topk(tp, s)); }
             fp.ids = rp.ids; fp.w64 = tp.w64; fp.S = tables->S; fp.L = tables->L; fp.h = tables->h;
             fp.st_pool = rp.st_pool; fp.st_target = rp.st_target; fp.st_scale = rp.st_scale;
             fp.B = (int)B; fp.N = N; fp.K = K; fp.M = pool_m; fp.n_shared = l.n_shared; fp.d = d; fp.I = I; fp.a_rows = ar;
@@ -854,7 +891,8 @@ static int decode_impl(const exfold_layer* layer, const void* x, const float* lo
         // a token has at most as many rows as the pool has experts
         const int64_t rows = B * std::min(K, (int)pool_m) + B * l.n_shared;
         rp.tile_rows = ffn_f32_tile_rows(rows, max_groups, d, I, sm_count());
-        const bool routed = ffn_f32_routes(true, B, rows, max_groups, N, K, d, I, rp.tile_rows, sm_count());
+        if (given) { rp.in_ids = given->ids; rp.in_w = given->w; }
+        const bool routed = !given && ffn_f32_routes(true, B, rows, max_groups, N, K, d, I, rp.tile_rows, sm_count());
         if (!routed) { ProfScope ps(6, s); EXFOLD_CUDA(launch_decode_route(rp, s)); }
         FfnF32Params fp = f32_params(x, w_gate, w_up, w_down, d, I, max_groups, rp.tile_rows);
         fp.offsets = rp.grp_off; fp.tile_start = rp.grp_tiles; fp.grp_expert = rp.grp_expert; fp.n_groups_dev = rp.n_groups;
@@ -880,6 +918,16 @@ int exfold_moe_decode(const exfold_layer* layer, const void* x, const float* log
                       const exfold_decode_meta* meta, void* ws, size_t ws_bytes, void* cuda_stream) {
     return decode_impl(layer, x, logits, B, w_gate, w_up, w_down, tables, nullptr, pool_m, y, meta, ws, ws_bytes,
                        cuda_stream);
+}
+
+int exfold_moe_decode_routed(const exfold_layer* layer, const void* x, const int32_t* ids, const float* w, int64_t B,
+                             const void* w_gate, const void* w_up, const void* w_down, const exfold_tables* tables,
+                             int32_t pool_m, void* y, const exfold_decode_meta* meta, void* ws, size_t ws_bytes,
+                             void* cuda_stream) {
+    if (!ids || ((reinterpret_cast<uintptr_t>(ids) | reinterpret_cast<uintptr_t>(w)) & 3) != 0) return EXFOLD_ERR_INVALID_ARG;
+    const GivenRoutes given{ids, w};
+    return decode_impl(layer, x, nullptr, B, w_gate, w_up, w_down, tables, nullptr, pool_m, y, meta, ws, ws_bytes, cuda_stream,
+                       nullptr, &given);
 }
 
 int exfold_moe_decode_static(const exfold_layer* layer, const void* x, const float* logits, int64_t B,
@@ -1115,6 +1163,51 @@ int exfold_router_logits(const exfold_layer* layer, const void* x, const void* w
                           true);
 }
 
+// Arguments of the two routing calls that they share
+static int route_check(const exfold_layer* layer, const float* logits, int64_t T, const exfold_router* r, const int32_t* ids) {
+    if (!valid_layer(layer) || !r || T < 0 || T > (int64_t)1 << 24 || (T > 0 && (!logits || !ids))) return EXFOLD_ERR_INVALID_ARG;
+    if (r->score != EXFOLD_SCORE_SOFTMAX && r->score != EXFOLD_SCORE_SIGMOID) return EXFOLD_ERR_INVALID_ARG;
+    if (!std::isfinite(r->scale)) return EXFOLD_ERR_INVALID_ARG;
+    const uintptr_t bits = reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(ids) | reinterpret_cast<uintptr_t>(r->bias);
+    return (bits & 3) != 0 ? EXFOLD_ERR_INVALID_ARG : EXFOLD_OK;
+}
+
+int exfold_route(const exfold_layer* layer, const float* logits, int64_t T, const exfold_router* router, int32_t* ids,
+                 float* w, int32_t* load, void* cuda_stream) {
+    int rc = route_check(layer, logits, T, router, ids);
+    if (rc != EXFOLD_OK) return rc;
+    const int N = layer->n_experts, K = layer->top_k, G = router->n_groups;
+    if ((T > 0 && !w) || ((reinterpret_cast<uintptr_t>(w) | reinterpret_cast<uintptr_t>(load)) & 3) != 0) return EXFOLD_ERR_INVALID_ARG;
+    if (router->group_score != EXFOLD_GROUP_MAX && router->group_score != EXFOLD_GROUP_TOP2) return EXFOLD_ERR_INVALID_ARG;
+    if (G < 1 || G > 32 || N % G != 0 || router->top_groups < 1 || router->top_groups > G || router->top_groups * (N / G) < K)
+        return EXFOLD_ERR_INVALID_ARG;
+    RouteGeneralParams p{};
+    p.logits = logits; p.bias = router->bias; p.T = T; p.N = N; p.K = K;
+    p.softmax = router->score == EXFOLD_SCORE_SOFTMAX;
+    p.n_groups = router->top_groups == G ? 1 : G;  // all groups stay: no groups
+    p.top_groups = router->top_groups;
+    p.group_top2 = router->group_score == EXFOLD_GROUP_TOP2 && N / G > 1;
+    p.by_score = router->bias != nullptr || (p.n_groups > 1 && p.group_top2);
+    p.renormalise = router->renormalise != 0; p.scale = router->scale;
+    p.ids = ids; p.w = w; p.load = load;
+    EXFOLD_CUDA(launch_route_general(p, sm_count(), reinterpret_cast<cudaStream_t>(cuda_stream)));
+    return EXFOLD_OK;
+}
+
+int exfold_route_backward(const exfold_layer* layer, const float* logits, const int32_t* ids, const float* dw, int64_t T,
+                          const exfold_router* router, float* dlogits, void* cuda_stream) {
+    int rc = route_check(layer, logits, T, router, ids);
+    if (rc != EXFOLD_OK) return rc;
+    if ((T > 0 && (!dw || !dlogits)) || ((reinterpret_cast<uintptr_t>(dw) | reinterpret_cast<uintptr_t>(dlogits)) & 3) != 0)
+        return EXFOLD_ERR_INVALID_ARG;
+    RouteBackwardParams p{};
+    p.logits = logits; p.ids = ids; p.dw = dw; p.T = T; p.N = layer->n_experts; p.K = layer->top_k;
+    p.softmax = router->score == EXFOLD_SCORE_SOFTMAX; p.renormalise = router->renormalise != 0; p.scale = router->scale;
+    p.dlogits = dlogits;
+    EXFOLD_CUDA(launch_route_backward(p, sm_count(), reinterpret_cast<cudaStream_t>(cuda_stream)));
+    return EXFOLD_OK;
+}
+
 int exfold_moe_prefill_layer(const exfold_layer* layer, const void* x, const void* w_router, int64_t T,
                              const void* w_gate, const void* w_up, const void* w_down, const exfold_tables* tables,
                              int32_t k_pre, float* logits, void* y, const exfold_prefill_meta* meta, void* ws,
@@ -1141,6 +1234,43 @@ int exfold_moe_decode_layer(const exfold_layer* layer, const void* x, const void
     if ((reinterpret_cast<uintptr_t>(logits) & 15) != 0 || !aligned16(w_router)) return EXFOLD_ERR_INVALID_ARG;
     return decode_impl(layer, x, logits, B, w_gate, w_up, w_down, tables, nullptr, pool_m, y, meta, ws, ws_bytes,
                        cuda_stream, w_router);
+}
+
+static bool valid_linear(const exfold_linear_desc* d) {
+    if (!d) return false;
+    const int64_t most = (int64_t)1 << 24;
+    if (d->in_features < 1 || d->in_features > most || d->out_features < 1 || d->out_features > most) return false;
+    if (d->dtype != EXFOLD_F32 && d->dtype != EXFOLD_BF16) return false;
+    if (d->out_dtype != EXFOLD_F32 && !(d->out_dtype == EXFOLD_BF16 && d->dtype == EXFOLD_BF16)) return false;
+    if (d->activation < EXFOLD_ACT_NONE || d->activation > EXFOLD_ACT_SILU) return false;
+    auto ld = [](int64_t v, int64_t row) { return v == 0 || (v >= row && v <= (int64_t)1 << 31); };
+    return ld(d->ldx, d->in_features) && ld(d->ldw, d->in_features) && ld(d->ldy, d->out_features) && ld(d->ldr, d->out_features);
+}
+
+size_t exfold_linear_workspace_bytes(const exfold_linear_desc* desc, int64_t max_tokens) {
+    if (!valid_linear(desc) || max_tokens < 0 || max_tokens > (int64_t)1 << 24) return 0;
+    return sizeof(DeviceStatus);
+}
+
+int exfold_linear(const exfold_linear_desc* desc, const void* x, const void* w, const void* bias, const void* residual,
+                  int64_t T, void* y, void* ws, size_t ws_bytes, void* cuda_stream) {
+    if (!valid_linear(desc) || !w || !ws || T < 0 || T > (int64_t)1 << 24 || (T > 0 && (!x || !y))) return EXFOLD_ERR_INVALID_ARG;
+    const bool bf16 = desc->dtype == EXFOLD_BF16, out_bf16 = desc->out_dtype == EXFOLD_BF16;
+    const uintptr_t el = bf16 ? 1 : 3, eo = out_bf16 ? 1 : 3;  // masks of the elements' own alignment
+    auto bits = [](const void* p) { return reinterpret_cast<uintptr_t>(p); };
+    if (((bits(x) | bits(w) | bits(bias)) & el) != 0 || ((bits(y) | bits(residual)) & eo) != 0 || (bits(ws) & 255) != 0)
+        return EXFOLD_ERR_INVALID_ARG;
+    LinearParams p{};
+    p.x = x; p.w = w; p.bias = bias; p.residual = residual; p.y = y; p.T = T;
+    p.K = (int)desc->in_features; p.N = (int)desc->out_features; p.act = desc->activation;
+    p.ldx = desc->ldx ? desc->ldx : p.K; p.ldw = desc->ldw ? desc->ldw : p.K;
+    p.ldy = desc->ldy ? desc->ldy : p.N; p.ldr = desc->ldr ? desc->ldr : p.N;
+    if (residual == y && p.ldr != p.ldy && T > 1) return EXFOLD_ERR_INVALID_ARG;
+    if (ws_bytes < exfold_linear_workspace_bytes(desc, T)) return EXFOLD_ERR_WORKSPACE_TOO_SMALL;
+    if (T == 0) return EXFOLD_OK;
+    p.status = at<DeviceStatus>(ws, 0);
+    EXFOLD_CUDA(launch_linear_simt(p, bf16, out_bf16, sm_count(), reinterpret_cast<cudaStream_t>(cuda_stream)));
+    return EXFOLD_OK;
 }
 
 int exfold_moe_prefill_host(const exfold_layer* layer, const void* x_host, const float* logits_host, int64_t T,

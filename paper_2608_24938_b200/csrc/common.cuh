@@ -226,8 +226,42 @@ struct PrefillScatterParams {
     int zero_words;
 };
 
+// Prefill on given routes: Eq. 10 ranks by in_w h, the folded weights start from in_w (route_given.cu)
+struct PrefillGivenParams {
+    PrefillRouteParams r;   // logits, lnh unused
+    const int32_t* in_ids;  // [T][K]
+    const float* in_w;      // [T][K]
+    const float* h;         // [N]; not read where nothing is folded
+};
+cudaError_t launch_prefill_given(PrefillGivenParams p, cudaStream_t s);
 cudaError_t launch_prefill_route(PrefillRouteParams p, cudaStream_t s);
 cudaError_t launch_prefill_scatter(PrefillScatterParams p, cudaStream_t s);
+
+// ---------------------------------------------------------------- routing by a model's own router (route_general.cu)
+struct RouteGeneralParams {
+    const float* logits;  // [T][N]
+    const float* bias;    // [N] or null
+    int64_t T;
+    int N, K;
+    int softmax, by_score;  // by_score: choices are scores (+ bias); else the logits, in the same order
+    int n_groups, top_groups, group_top2;
+    int renormalise;
+    float scale;
+    int32_t* ids;   // [T][K]
+    float* w;       // [T][K]
+    int32_t* load;  // [N] or null
+};
+struct RouteBackwardParams {
+    const float* logits;  // [T][N]
+    const int32_t* ids;   // [T][K]
+    const float* dw;      // [T][K]
+    int64_t T;
+    int N, K, softmax, renormalise;
+    float scale;
+    float* dlogits;  // [T][N]
+};
+cudaError_t launch_route_general(const RouteGeneralParams& p, int sms, cudaStream_t s);
+cudaError_t launch_route_backward(const RouteBackwardParams& p, int sms, cudaStream_t s);
 
 // ---------------------------------------------------------------- routing (decode)
 struct DecodeRouteParams {
@@ -258,6 +292,9 @@ struct DecodeRouteParams {
     int32_t* slot_row;    // [B][K] row of each routed slot, -1 for a slot merged into an earlier one
     int32_t* n_groups;    // [3]: number of groups, total rows, first row of the shared expert's group
     DeviceStatus* status; // cleared here (first kernel of a decode call)
+    // given routes [B][K] in the place of the logits, or null
+    const int32_t* in_ids;
+    const float* in_w;
 };
 cudaError_t launch_decode_route(const DecodeRouteParams& p, cudaStream_t s);
 
@@ -274,6 +311,8 @@ struct DecodeTopkParams {
     DeviceStatus* status;
 };
 cudaError_t launch_decode_topk(const DecodeTopkParams& p, cudaStream_t s);
+// Given routes [B][K] in the form that launch_decode_topk leaves (p.ids, p.w64; clears the status record)
+cudaError_t launch_decode_given(const DecodeTopkParams& p, const int32_t* in_ids, const float* in_w, cudaStream_t s);
 
 // Decode, bf16 layers: the gate/up half of the expert FFN over the pool. The kernel finishes the routing in its
 // prologue (every CTA: pool of Eq. 11 from the routed weights, minimum-loss targets of Eq. 12, remap of Eq. 14,
@@ -430,6 +469,20 @@ cudaError_t launch_combine_rows(const __nv_bfloat16* O, const int32_t* inv_pos, 
                                 int n_shared, const int32_t* shared0_dev, int parts, int64_t part_rows,
                                 __nv_bfloat16* y, cudaStream_t s);
 constexpr int kMaxDecodeKsplit = 2;
+
+// ---------------------------------------------------------------- dense products with an epilogue
+struct LinearParams {
+    const void* x;         // [T][K], rows ldx elements apart
+    const void* w;         // [N][K]
+    const void* bias;      // [N] or null, in the type of x and w
+    const void* residual;  // [T][N] or null, in the type of y
+    void* y;               // [T][N]
+    int64_t T;
+    int K, N, act;
+    int64_t ldx, ldw, ldy, ldr;
+    DeviceStatus* status;  // cleared by the call's first kernel
+};
+cudaError_t launch_linear_simt(const LinearParams& p, bool bf16, bool out_bf16, int sms, cudaStream_t s);
 
 // ---------------------------------------------------------------- calibration
 struct CalibStatsParams {

@@ -44,7 +44,7 @@ __device__ __forceinline__ void cp_async4(void* smem_dst, const void* gmem_src) 
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(ptx::smem_u32(smem_dst)), "l"(gmem_src) : "memory");
 }
 
-template <int NPL>
+template <int NPL, bool GIVEN>  // GIVEN: the routes are the caller's (NPL unused)
 __global__ void __launch_bounds__(kDecThreads) decode_route_kernel(DecodeRouteParams p) {
     extern __shared__ __align__(16) unsigned char smraw[];
     DecSmem& sm = *reinterpret_cast<DecSmem*>(smraw);
@@ -79,10 +79,12 @@ __global__ void __launch_bounds__(kDecThreads) decode_route_kernel(DecodeRoutePa
     // double; the first token's logits are requested before the table rows so that they arrive first.
     const int i_first = rank + nct * warp, i_step = nct * kWarps;
     float vn[NPL];
+    if constexpr (!GIVEN) {
 #pragma unroll
-    for (int q = 0; q < NPL; ++q) {
-        const int e = lane + 32 * q;
-        vn[q] = (i_first < B && e < N) ? p.logits[(size_t)i_first * N + e] : -INFINITY;
+        for (int q = 0; q < NPL; ++q) {
+            const int e = lane + 32 * q;
+            vn[q] = (i_first < B && e < N) ? p.logits[(size_t)i_first * N + e] : -INFINITY;
+        }
     }
     if (!is_static) {
         // Rows [s_lo, s_hi) of L and S and the norm table, needed once the sums are in: asynchronous copies
@@ -97,43 +99,52 @@ __global__ void __launch_bounds__(kDecThreads) decode_route_kernel(DecodeRoutePa
         for (int e = threadIdx.x; e < N; e += kDecThreads) cp_async4(&sm.hh[e], p.h + e);
     }
     for (int i = i_first; i < B; i += i_step) {
-        uint32_t key_q[NPL];
-        uint32_t used = 0;
-#pragma unroll
-        for (int q = 0; q < NPL; ++q) {
-            key_q[q] = float_order_key(vn[q]);
-            if (lane + 32 * q >= N) used |= 1u << q;
-        }
-#pragma unroll
-        for (int q = 0; q < NPL; ++q) {
-            const int e = lane + 32 * q;
-            vn[q] = (i + i_step < B && e < N) ? p.logits[(size_t)(i + i_step) * N + e] : -INFINITY;
-        }
         int my_id = -1;
-        float my_r = 0.f;
-        for (int k = 0; k < K; ++k) {
-            uint32_t bk = 0;
-            int be = 0x7fffffff;
+        double ex = 0.0, sum = 0.0;
+        if constexpr (GIVEN) {
+            if (lane < K) {
+                my_id = p.in_ids[(size_t)i * K + lane];
+                ex = (double)p.in_w[(size_t)i * K + lane];
+            }
+            sum = 1.0;
+            if (my_id < 0 || my_id >= N) my_id = 0, ex = 0.0;
+        } else {
+            uint32_t key_q[NPL];
+            uint32_t used = 0;
 #pragma unroll
             for (int q = 0; q < NPL; ++q) {
-                const bool free_q = !((used >> q) & 1u);
-                if (free_q && (be == 0x7fffffff || key_q[q] > bk)) {
-                    bk = key_q[q];
-                    be = lane + 32 * q;
+                key_q[q] = float_order_key(vn[q]);
+                if (lane + 32 * q >= N) used |= 1u << q;
+            }
+#pragma unroll
+            for (int q = 0; q < NPL; ++q) {
+                const int e = lane + 32 * q;
+                vn[q] = (i + i_step < B && e < N) ? p.logits[(size_t)(i + i_step) * N + e] : -INFINITY;
+            }
+            float my_r = 0.f;
+            for (int k = 0; k < K; ++k) {
+                uint32_t bk = 0;
+                int be = 0x7fffffff;
+#pragma unroll
+                for (int q = 0; q < NPL; ++q) {
+                    const bool free_q = !((used >> q) & 1u);
+                    if (free_q && (be == 0x7fffffff || key_q[q] > bk)) {
+                        bk = key_q[q];
+                        be = lane + 32 * q;
+                    }
+                }
+                uint32_t mk;
+                be = warp_argmax(be != 0x7fffffff, bk, be, &mk);
+                if ((be & 31) == lane) used |= 1u << (be >> 5);
+                if (lane == k) {
+                    my_id = be;
+                    my_r = float_from_order_key(mk);
                 }
             }
-            uint32_t mk;
-            be = warp_argmax(be != 0x7fffffff, bk, be, &mk);
-            if ((be & 31) == lane) used |= 1u << (be >> 5);
-            if (lane == k) {
-                my_id = be;
-                my_r = float_from_order_key(mk);
-            }
+            const float rmax = __shfl_sync(0xffffffffu, my_r, 0);
+            ex = lane < K ? exp((double)my_r - (double)rmax) : 0.0;
+            for (int k = 0; k < K; ++k) sum += __shfl_sync(0xffffffffu, ex, k);  // slot order, like the definition
         }
-        const float rmax = __shfl_sync(0xffffffffu, my_r, 0);
-        double ex = lane < K ? exp((double)my_r - (double)rmax) : 0.0;
-        double sum = 0.0;
-        for (int k = 0; k < K; ++k) sum += __shfl_sync(0xffffffffu, ex, k);  // slot order, like the definition
         if (!cleared) {  // warp-uniform
             cluster.barrier_wait();
             cleared = true;
@@ -502,7 +513,25 @@ __global__ void __launch_bounds__(256) static_pool_kernel(int N, int M, const fl
     }
 }
 
+// Given routes as the top-k kernel leaves its own: the weights in double, an id that is no expert as expert 0 with weight 0
+__global__ void __launch_bounds__(256) decode_given_kernel(DecodeTopkParams p, const int32_t* __restrict__ in_ids,
+                                                           const float* __restrict__ in_w) {
+    grid_dep_launch();
+    grid_dep_wait();
+    if (blockIdx.x == 0 && threadIdx.x < 4) reinterpret_cast<int*>(p.status)[threadIdx.x] = 0;
+    const int s = blockIdx.x * 256 + threadIdx.x;
+    if (s >= p.B * p.K) return;
+    const int id = in_ids[s];
+    const bool ok = id >= 0 && id < p.N;
+    p.ids[s] = ok ? id : 0;
+    p.w64[s] = ok ? (double)in_w[s] : 0.0;
+}
+
 }  // namespace
+
+cudaError_t launch_decode_given(const DecodeTopkParams& p, const int32_t* in_ids, const float* in_w, cudaStream_t s) {
+    return launch_pdl(decode_given_kernel, (unsigned)(p.B * p.K + 255) / 256, 256, 0, s, p, in_ids, in_w);
+}
 
 cudaError_t launch_decode_route(const DecodeRouteParams& p, cudaStream_t s) {
     const int npl = (p.N + 31) / 32;
@@ -513,15 +542,19 @@ cudaError_t launch_decode_route(const DecodeRouteParams& p, cudaStream_t s) {
     // state + this CTA's rows of the two tables
     const size_t smem = kDecSmemBytes + 2 * (size_t)((p.N + ncl - 1) / ncl) * p.N * sizeof(float);
     cudaError_t err = cudaSuccess;
-#define EXFOLD_DEC_LAUNCH(NPL)                                                                              \
-    err = ensure_smem(decode_route_kernel<NPL>, smem);                                                                  \
+#define EXFOLD_DEC_LAUNCH(...)                                                                              \
+    err = ensure_smem(decode_route_kernel<__VA_ARGS__>, smem);                                              \
     if (err != cudaSuccess) return err;                                                                     \
-    err = launch_pdl_cluster(decode_route_kernel<NPL>, ncl, kDecThreads, smem, ncl, s, p);
+    err = launch_pdl_cluster(decode_route_kernel<__VA_ARGS__>, ncl, kDecThreads, smem, ncl, s, p);
+    if (p.in_ids != nullptr) {
+        EXFOLD_DEC_LAUNCH(1, true)
+        return err;
+    }
     switch (npl) {
-        case 1: EXFOLD_DEC_LAUNCH(1) break;
-        case 2: EXFOLD_DEC_LAUNCH(2) break;
-        case 3: case 4: EXFOLD_DEC_LAUNCH(4) break;
-        default: EXFOLD_DEC_LAUNCH(8) break;
+        case 1: EXFOLD_DEC_LAUNCH(1, false) break;
+        case 2: EXFOLD_DEC_LAUNCH(2, false) break;
+        case 3: case 4: EXFOLD_DEC_LAUNCH(4, false) break;
+        default: EXFOLD_DEC_LAUNCH(8, false) break;
     }
 #undef EXFOLD_DEC_LAUNCH
     return err;

@@ -1,0 +1,202 @@
+"""The dense product with bias, activation and residual against the definition in 64 bits."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+ACTS = ["none", "relu", "gelu", "gelu_tanh", "silu"]
+
+
+@pytest.fixture(scope="module")
+def ex():
+    from paper_2608_24938_b200 import binding
+    return binding
+
+
+def act64(v, name):
+    if name == "relu":
+        return torch.relu(v)
+    if name == "gelu":
+        return 0.5 * v * torch.special.erfc(-v / math.sqrt(2))
+    if name == "gelu_tanh":
+        return 0.5 * v * (1 + torch.tanh(math.sqrt(2 / math.pi) * (v + 0.044715 * v ** 3)))
+    if name == "silu":
+        return v * torch.sigmoid(v)
+    return v
+
+
+def reference(x, w, bias, residual, act, out):
+    """(value, bound of the error). Products of bf16 are exact in fp32, of fp32 rounded; sums are taken in fp32, on the tensor cores
+    in steps of 16 products that may be cut off instead of rounded: (in / 8 + 16) 2^-23 of the sum of magnitudes there, and
+    (in + 2) 2^-24 of it where each product is added with one rounding. Activations have slopes up to 1.13 and are computed to
+    8 half steps of their argument; then the residual's addition and half a step of the output."""
+    X, W = x.double(), w.double()
+    K = x.shape[1]
+    pre = X @ W.T
+    mag = X.abs() @ W.abs().T
+    if bias is not None:
+        pre = pre + bias.double()
+        mag = mag + bias.double().abs()
+    steps = max((K / 8 + 16) * 2.0 ** -23 if x.dtype == torch.bfloat16 else 0.0, (K + 2) * 2.0 ** -24)
+    err = 1.13 * steps * mag + 8 * 2.0 ** -24 * pre.abs()
+    v = act64(pre, act)
+    if residual is not None:
+        err = err + 2.0 ** -24 * (v.abs() + residual.double().abs())
+        v = v + residual.double()
+    half = 2.0 ** -8 if out == torch.bfloat16 else 2.0 ** -24
+    return v, err + half * (v.abs() + err) + 2.0 ** -126
+
+
+def rows(r, c, dtype, seed, std=1.0, ld=None, offset=0):
+    """r x c with rows ld elements apart, `offset` elements into a buffer; what lies between and around holds NaN."""
+    g = torch.Generator().manual_seed(seed)
+    ld = c if ld is None else ld
+    buf = torch.full((offset + r * ld + 64,), float("nan"), dtype=dtype)
+    view = buf[offset:offset + r * ld].view(r, ld)[:, :c]
+    view.copy_((torch.randn((r, c), generator=g) * std).to(dtype))
+    dev = buf.cuda()
+    return dev[offset:offset + r * ld].view(r, ld)[:, :c], dev
+
+
+def check(ex, T, i, o, dtype=torch.bfloat16, out=None, bias=True, residual=True, act="none", ldx=None, ldw=None, ldy=None, ldr=None,
+          offset=0, in_place=False, seed=0):
+    out = dtype if out is None else out
+    x, _ = rows(T, i, dtype, seed + 1, ld=ldx, offset=offset)
+    w, _ = rows(o, i, dtype, seed + 2, std=i ** -0.5, ld=ldw, offset=offset)
+    b = rows(1, o, dtype, seed + 3, offset=offset)[0][0] if bias else None
+    y, ybuf = rows(T, o, out, seed + 4, ld=ldy, offset=offset)
+    r = None
+    if residual:
+        r = y if in_place else rows(T, o, out, seed + 5, ld=ldr, offset=offset)[0]
+    ref, bound = reference(x, w, b, r, act, out)
+    if not in_place:
+        y.fill_(float("nan"))
+    around = torch.ones_like(ybuf, dtype=torch.bool)
+    around[offset:offset + T * (ldy or o)].view(T, ldy or o)[:, :o] = False
+    ws = ex.alloc_linear_workspace(i, o, T, dtype, out)
+    ws.fill_(0xFF)
+    ex.exfold_linear(x, w, y, ws, bias=b, residual=r, activation=act)
+    assert ex.exfold_device_status(ws) == 0
+    assert ybuf[around].isnan().all(), "something beside the rows was written"
+    got = y.double()
+    assert got.isfinite().all()
+    bad = (got - ref).abs() > bound
+    assert not bad.any(), f"{int(bad.sum())} of {bad.numel()} outside the bound, worst {float(((got - ref).abs() / bound).max()):.2f}"
+    return y
+
+
+TOKENS = [1, 2, 3, 7, 8, 9, 15, 16, 17, 31, 33, 64, 65, 100, 127, 128, 129, 200, 256, 257, 300, 513]
+
+
+@pytest.mark.parametrize("T", TOKENS)
+@pytest.mark.parametrize("i,o", [(64, 64), (128, 256), (256, 40), (1024, 520), (2048, 768)])
+def test_linear_bf16(ex, T, i, o):
+    check(ex, T, i, o, act="silu")
+    check(ex, T, i, o, out=torch.float32, bias=False, act="gelu")
+
+
+@pytest.mark.parametrize("T", [1, 5, 12, 64, 130, 300, 700])
+@pytest.mark.parametrize("i,o", [(8, 1), (1, 8), (1, 1), (72, 7), (136, 129), (200, 333), (1000, 1411), (2040, 257), (63, 65), (517, 100),
+                                 (6591, 64)])
+def test_linear_odd_sizes(ex, T, i, o):
+    pad = (i + 7) // 8 * 8 + 8
+    check(ex, T, i, o, act="gelu_tanh")
+    check(ex, T, i, o, ldx=pad, ldw=pad, ldy=o + 3, ldr=o + 5, act="relu")
+    check(ex, T, i, o, out=torch.float32, ldx=pad, ldw=pad + 8, ldy=o + 1)
+
+
+@pytest.mark.parametrize("dtype,out", [(torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32)])
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("bias,residual", [(False, False), (True, False), (False, True), (True, True)])
+def test_linear_epilogues(ex, dtype, out, act, bias, residual):
+    for T in (1, 20, 300):
+        check(ex, T, 192, 264, dtype, out, bias, residual, act)
+
+
+@pytest.mark.parametrize("T", [1, 2, 9, 64, 100, 257, 1000])
+@pytest.mark.parametrize("i,o", [(1, 1), (3, 5), (128, 256), (100, 129), (517, 64), (768, 2048)])
+def test_linear_f32(ex, T, i, o):
+    check(ex, T, i, o, torch.float32, act="silu")
+    check(ex, T, i, o, torch.float32, ldx=i + 1, ldw=i + 3, ldy=o + 1, ldr=o, act="none")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T", [1, 6, 40, 200, 600])
+@pytest.mark.parametrize("offset", [1, 4, 8])
+def test_linear_unaligned_operands(ex, dtype, T, offset):
+    """Operands that start anywhere in a buffer, dense and with odd row distances."""
+    check(ex, T, 264, 136, dtype, offset=offset, act="relu")
+    check(ex, T, 264, 136, dtype, offset=offset, ldx=267, ldw=265, ldy=137, ldr=139)
+    check(ex, T, 265, 135, dtype, offset=offset)
+
+
+@pytest.mark.parametrize("dtype,out", [(torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32)])
+@pytest.mark.parametrize("T", [1, 8, 33, 129, 520])
+def test_linear_in_place_residual(ex, dtype, out, T):
+    check(ex, T, 256, 512, dtype, out, in_place=True, act="gelu")
+    check(ex, T, 256, 500, dtype, out, in_place=True, ldy=504)
+
+
+@pytest.mark.parametrize("T,i,o", [(2048, 4096, 1408), (1300, 2048, 4096), (4096, 768, 2048), (300, 4096, 14336), (5, 4096, 14336),
+                                   (16, 14336, 4096), (777, 2040, 1411)])
+def test_linear_large(ex, T, i, o):
+    check(ex, T, i, o, act="gelu_tanh")
+
+
+def test_linear_zero_tokens_writes_nothing(ex):
+    w = torch.ones((8, 64), dtype=torch.bfloat16, device="cuda")
+    ws = ex.alloc_linear_workspace(64, 8, 0, torch.bfloat16)
+    ex.exfold_linear(w[:0], w, torch.empty((0, 8), dtype=torch.bfloat16, device="cuda"), ws)
+
+
+@pytest.mark.parametrize("T", [1, 16, 130, 700])
+def test_linear_rows_do_not_mix(ex, T):
+    """An infinity or NaN in one token's row stays there; weights of unused columns do too."""
+    x, _ = rows(T, 256, torch.bfloat16, 1)
+    w, _ = rows(264, 256, torch.bfloat16, 2)
+    ws = ex.alloc_linear_workspace(256, 264, T, torch.bfloat16)
+    y0, y1 = (torch.empty((T, 264), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    ex.exfold_linear(x, w, y0, ws)
+    w2, x2 = w.clone(), x.clone()
+    w2[3, 5] = float("inf")
+    x2[T - 1, 7] = float("nan")
+    ex.exfold_linear(x2, w2, y1, ws)
+    keep = torch.arange(264, device="cuda") != 3
+    assert torch.equal(y0[:T - 1, keep], y1[:T - 1, keep])
+    assert y1[T - 1].isnan().all() and not y1[:T - 1, 3].isfinite().any()
+
+
+@pytest.mark.parametrize("T", [1, 24, 200, 1500])
+def test_linear_is_reproducible_and_captured(ex, T):
+    i, o = 1024, 768
+    x, _ = rows(T, i, torch.bfloat16, 1)
+    w, _ = rows(o, i, torch.bfloat16, 2)
+    ws, ws2 = (ex.alloc_linear_workspace(i, o, T, torch.bfloat16) for _ in range(2))
+    y, y2, ref = (torch.empty((T, o), dtype=torch.bfloat16, device="cuda") for _ in range(3))
+    ex.exfold_linear(x, w, ref, ws)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        ex.exfold_linear(x, w, y, ws)
+        ex.exfold_linear(x, w, y2, ws2)
+    for _ in range(3):
+        y.zero_(), y2.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, ref) and torch.equal(y2, ref)
+    # two streams at once, a workspace each
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    y.zero_(), y2.zero_()
+    torch.cuda.synchronize()
+    for _ in range(4):
+        ex.exfold_linear(x, w, y, ws, stream=a)
+        ex.exfold_linear(x, w, y2, ws2, stream=b)
+    torch.cuda.synchronize()
+    assert torch.equal(y, ref) and torch.equal(y2, ref)
+    # new inputs right before the call, on the call's stream
+    with torch.cuda.stream(a):
+        x.mul_(2.0)
+        ex.exfold_linear(x, w, y, ws, stream=a)
+    torch.cuda.synchronize()
+    assert torch.equal(y, ref * 2)
