@@ -148,12 +148,12 @@ EncodeTiledFn encode_fn() {
 
 constexpr int kMaxHostChunks = 4;  // host-buffer prefill: chunks of >= 2048 tokens in flight
 
-// bf16 matrix [rows][cols] row-major; box = box_rows x kGemmBK columns, 128-byte swizzle (a box row)
-bool make_tmap(CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows) {
+// bf16 matrix [rows][cols] row-major, rows ld elements apart (0: dense); box = box_rows x kGemmBK columns, 128-byte swizzle (a box row)
+bool make_tmap(CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows, uint64_t ld = 0) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     cuuint64_t dims[2] = {cols, rows};
-    cuuint64_t strides[1] = {cols * 2};
+    cuuint64_t strides[1] = {(ld ? ld : cols) * 2};
     cuuint32_t box[2] = {(cuuint32_t)kGemmBK, box_rows};
     cuuint32_t estr[2] = {1, 1};
     CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
@@ -1269,7 +1269,27 @@ int exfold_linear(const exfold_linear_desc* desc, const void* x, const void* w, 
     if (ws_bytes < exfold_linear_workspace_bytes(desc, T)) return EXFOLD_ERR_WORKSPACE_TOO_SMALL;
     if (T == 0) return EXFOLD_OK;
     p.status = at<DeviceStatus>(ws, 0);
-    EXFOLD_CUDA(launch_linear_simt(p, bf16, out_bf16, sm_count(), reinterpret_cast<cudaStream_t>(cuda_stream)));
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
+    PdlScope pdl_scope(true);
+    if (bf16 && aligned16(x) && aligned16(w) && ((p.ldx | p.ldw) & 7) == 0) {
+        const int64_t items = ((T + 255) / 256) * ((p.N + 255) / 256);
+        if (items >= sm_count() / 2) {
+            LinearPairParams q{};
+            q.l = p;
+            if (!make_tmap(&q.tm_x, x, (uint64_t)T, p.K, 128, p.ldx) || !make_tmap(&q.tm_w, w, (uint64_t)p.N, p.K, 128, p.ldw))
+                return EXFOLD_ERR_CUDA;
+            EXFOLD_CUDA(launch_linear_pair(q, out_bf16, sm_count(), s));
+        } else {
+            LinearTileParams q{};
+            q.l = p;
+            q.plan = linear_tile_plan(T, p.N, p.K, sm_count());
+            if (!make_tmap(&q.tm_x, x, (uint64_t)T, p.K, q.plan.a_rows, p.ldx) || !make_tmap(&q.tm_w, w, (uint64_t)p.N, p.K, q.plan.bn, p.ldw))
+                return EXFOLD_ERR_CUDA;
+            EXFOLD_CUDA(launch_linear_tile(q, out_bf16, s));
+        }
+        return EXFOLD_OK;
+    }
+    EXFOLD_CUDA(launch_linear_simt(p, bf16, out_bf16, sm_count(), s));
     return EXFOLD_OK;
 }
 

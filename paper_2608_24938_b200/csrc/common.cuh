@@ -483,6 +483,27 @@ struct LinearParams {
     DeviceStatus* status;  // cleared by the call's first kernel
 };
 cudaError_t launch_linear_simt(const LinearParams& p, bool bf16, bool out_bf16, int sms, cudaStream_t s);
+// bf16 on the tensor cores, K split over a cluster (linear_tile.cu)
+struct LinearTilePlan {
+    int a_rows, bn, split, stages;  // token rows and features per tile, CTAs per tile, ring
+    size_t smem;
+};
+LinearTilePlan linear_tile_plan(int64_t T, int N, int K, int sms);
+struct LinearTileParams {
+    LinearParams l;
+    CUtensorMap tm_x;  // x, box a_rows x 64
+    CUtensorMap tm_w;  // w, box bn x 64
+    LinearTilePlan plan;
+};
+cudaError_t launch_linear_tile(const LinearTileParams& p, bool out_bf16, cudaStream_t s);
+// on CTA pairs, 256 tokens x 256 features per pair (linear_pair.cu)
+struct LinearPairParams {
+    LinearParams l;
+    CUtensorMap tm_x;  // box 128 x 64
+    CUtensorMap tm_w;  // box 128 x 64
+    int mt, nt, band;  // tiles; row tiles that share a weight tile in a run of the work order
+};
+cudaError_t launch_linear_pair(LinearPairParams p, bool out_bf16, int sms, cudaStream_t s);
 
 // ---------------------------------------------------------------- calibration
 struct CalibStatsParams {

@@ -12,18 +12,6 @@ namespace {
 constexpr int kLsThreads = 256;
 constexpr int kLsBK = 16;
 
-__device__ __forceinline__ float to_f32(float v) { return v; }
-__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ void load4(const float* p, float (&v)[4]) {
-    const float4 t = *reinterpret_cast<const float4*>(p);
-    v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
-}
-__device__ __forceinline__ void load4(const __nv_bfloat16* p, float (&v)[4]) {
-    const uint2 t = *reinterpret_cast<const uint2*>(p);
-    const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&t.x));
-    const float2 b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&t.y));
-    v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
-}
 // Two products at once: the packed form issues half as many instructions
 __device__ __forceinline__ void fma2(float2& c, const float2& a, const float2& b) {
     asm("fma.rn.f32x2 %0, %1, %2, %0;"
@@ -55,11 +43,12 @@ __global__ void __launch_bounds__(kLsThreads) linear_simt_kernel(LinearParams p)
         if (row >= rows) return;
         const T* src = base + row * ld + k;
         if (VEC && k + 4 <= p.K) {
-            load4(src, v);
+            const float4 t = linear_load4(src);
+            v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (k + j < p.K) v[j] = to_f32(src[j]);
+                if (k + j < p.K) v[j] = linear_f32(src[j]);
         }
     };
     auto load = [&](int k0) {
@@ -132,13 +121,13 @@ __global__ void __launch_bounds__(kLsThreads) linear_simt_kernel(LinearParams p)
     for (int j = 0; j < TN; ++j) {
         const int n = n0 + (j >> 2) * 64 + tx * 4 + (j & 3);
         if (n >= p.N) continue;
-        const float bv = bias != nullptr ? to_f32(bias[n]) : 0.f;
+        const float bv = bias != nullptr ? linear_f32(bias[n]) : 0.f;
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             const int64_t m = m0 + (i >> 2) * 64 + ty * 4 + (i & 3);
             if (m >= p.T) continue;
             float v = linear_act(((j & 1) ? acc[i][j / 2].y : acc[i][j / 2].x) + bv, p.act);
-            if (r != nullptr) v += to_f32(r[m * p.ldr + n]);
+            if (r != nullptr) v += linear_f32(r[m * p.ldr + n]);
             linear_store(y + m * p.ldy + n, v);
         }
     }

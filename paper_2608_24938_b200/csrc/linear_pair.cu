@@ -1,0 +1,253 @@
+// Dense product with epilogue, bf16 operands, many tokens: CTA pairs (tcgen05 cta_group::2), 256 tokens x 256 features per pair.
+//
+// A pair's k-block (K = 64) needs 32 KB per SM for 512 cycles of the tensor pipe, what an SM takes in from L2; a single CTA's
+// 128 x 256 tile needs 48 KB for the same. Six stages of 32 KB are in flight, two 256-column accumulators hand a finished tile to the
+// epilogue warps while the next one is multiplied. Roles per CTA: warps 0 and 1 TMA producers (k-blocks dealt in turn; own token
+// rows, own half of the weight rows, both CTAs' bytes counted on the leader's barrier), warp 2 MMA issuer (leader), the other eight
+// epilogue: two per quadrant of the accumulator's lanes, half of the columns each. An epilogue warp passes 32 columns at a time
+// through shared memory so that residual and result move in whole rows of 64 or 128 bytes.
+#include <algorithm>
+
+#include "common.cuh"
+#include "linear_epilogue.cuh"
+#include "ptx.cuh"
+
+namespace exfold {
+
+namespace {
+
+constexpr int kLpBK = kGemmBK;
+constexpr int kLpStages = 6;
+constexpr int kLpTileBytes = kTileM * kLpBK * 2;  // 16 KB: this CTA's token rows, or its half of the weight rows
+constexpr int kLpStageBytes = 2 * kLpTileBytes;
+constexpr int kLpEpiWarps = 8;
+constexpr int kLpChunk = 16;                           // accumulator columns per trip through shared memory
+constexpr int kLpOutBytes = 32 * kLpChunk * 4;         // per epilogue warp
+constexpr int kLpSmem = kLpStages * kLpStageBytes + kLpEpiWarps * kLpOutBytes + 1024;
+constexpr int kLpThreads = 32 * (3 + kLpEpiWarps);
+constexpr int kLpTmemCols = 512;
+
+// Work order: bands of row tiles; within a band the feature tiles, each against all row tiles of the band
+__device__ __forceinline__ void decode_tile(const LinearPairParams& p, int w, int* m, int* n) {
+    const int per = p.band * p.nt, b = w / per, left = w - b * per;
+    const int rows = min(p.band, p.mt - b * p.band);
+    *n = left / rows;
+    *m = b * p.band + left - *n * rows;
+}
+
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+}
+
+template <typename O>
+__global__ void __launch_bounds__(kLpThreads, 1) linear_pair_kernel(const __grid_constant__ LinearPairParams p) {
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t full_bar[kLpStages];   // used in the leader
+    __shared__ __align__(8) uint64_t empty_bar[kLpStages];  // one per CTA, released by the leader's commits
+    __shared__ __align__(8) uint64_t tfull_bar[2];          // one per CTA
+    __shared__ __align__(8) uint64_t tempty_bar[2];         // used in the leader: the epilogue warps of both CTAs
+    __shared__ uint32_t tmem_base_s;
+    __shared__ int abort_s;
+    unsigned char* tiles =
+        reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    const int warp = ptx::warp_index(), lane = threadIdx.x & 31;
+    const int rank = (int)ptx::cluster_ctarank();  // 0 = leader
+    if (threadIdx.x == 0) {
+        ptx::prefetch_tmap(&p.tm_x);
+        ptx::prefetch_tmap(&p.tm_w);
+        for (int s = 0; s < kLpStages; ++s) {
+            ptx::mbar_init(&full_bar[s], 1);
+            ptx::mbar_init(&empty_bar[s], 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            ptx::mbar_init(&tfull_bar[s], 1);
+            ptx::mbar_init(&tempty_bar[s], 2 * kLpEpiWarps);
+        }
+        abort_s = 0;
+        ptx::fence_mbar_init();
+    }
+    if (warp == 2) {
+        ptx::tmem_alloc_pair(&tmem_base_s, kLpTmemCols);
+        ptx::tmem_relinquish_pair();
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::cluster_sync_all();  // both CTAs' barriers are initialised and their tensor memory allocated
+    ptx::tc_fence_after();
+    grid_dep_wait();
+    if (blockIdx.x == 0 && threadIdx.x < 4) reinterpret_cast<int*>(p.l.status)[threadIdx.x] = 0;
+    const uint32_t tmem_base = tmem_base_s;
+    volatile int* abort_flag = &abort_s;
+    const int nkb = (p.l.K + kLpBK - 1) / kLpBK, total = p.mt * p.nt;
+    const int w_begin = (int)blockIdx.x >> 1, w_stride = (int)gridDim.x >> 1;
+
+    if (warp < 2) {
+        // ------------------------------------------------ TMA producers (both CTAs; k-block c belongs to producer c % 2)
+        if (ptx::elect_one()) {
+            int stage = 0, phase = 0, turn = 0;
+            bool ok = true;
+            for (int w = w_begin; w < total && ok; w += w_stride) {
+                int m, n;
+                decode_tile(p, w, &m, &n);
+                const int arow = m * 256 + rank * kTileM, brow = n * 256 + rank * 128;
+                for (int kb = 0; kb < nkb; ++kb) {
+                    if (turn == warp) {
+                        if (!ptx::mbar_wait_local(&empty_bar[stage], phase ^ 1, abort_flag, p.l.status, 1)) {
+                            ok = false;
+                            break;
+                        }
+                        unsigned char* dst = tiles + stage * kLpStageBytes;
+                        if (rank == 0) ptx::mbar_expect_tx(&full_bar[stage], 2 * kLpStageBytes);  // both CTAs' bytes
+                        ptx::tma_load_2d_pair(dst, &p.tm_x, &full_bar[stage], kb * kLpBK, arow);
+                        ptx::tma_load_2d_pair(dst + kLpTileBytes, &p.tm_w, &full_bar[stage], kb * kLpBK, brow);
+                    }
+                    turn ^= 1;
+                    if (++stage == kLpStages) {
+                        stage = 0;
+                        phase ^= 1;
+                    }
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp == 2) {
+        // ------------------------------------------------ MMA issuer (leader CTA only)
+        if (rank == 0 && ptx::elect_one()) {
+            constexpr uint32_t idesc = ptx::make_idesc_bf16(256, 256);
+            const uint32_t lo0 = (ptx::smem_u32(tiles) & 0x3FFFFu) >> 4;
+            constexpr uint32_t lo_step = (uint32_t)kLpStageBytes >> 4, lo_b = (uint32_t)kLpTileBytes >> 4;
+            const uint32_t desc_hi = (uint32_t)(ptx::make_kmajor_sw128_desc(0) >> 32);
+            int stage = 0, phase = 0, iter = 0;
+            bool ok = true, ready = false;
+            static_assert(kLpStages == 6, "the k-loop below is written out for six ring stages");
+            for (int w = w_begin; w < total && ok; w += w_stride, ++iter) {
+                const int as = iter & 1, aphase = (iter >> 1) & 1;
+                if (!ptx::mbar_wait_local(&tempty_bar[as], aphase ^ 1, abort_flag, p.l.status, 2)) break;
+                ptx::tc_fence_after();
+                const uint32_t d_tmem = tmem_base + as * 256;
+                // written out once per ring stage: with the stage a compile-time constant a k-block costs this thread the MMA
+                // sequence, one compare and one branch
+                int kb = 0;
+#define EXFOLD_LP_KBLOCK(S)                                                                                        \
+    {                                                                                                               \
+        constexpr int NS = (S) + 1 == kLpStages ? 0 : (S) + 1;                                                      \
+        const uint32_t nphase = NS == 0 ? phase ^ 1 : phase;                                                        \
+        if (!ready && !ptx::mbar_wait_local(&full_bar[S], phase, abort_flag, p.l.status, 3)) {                      \
+            ok = false;                                                                                             \
+            break;                                                                                                  \
+        }                                                                                                           \
+        ready = ptx::umma_kblock_bf16_pair(d_tmem, lo0 + (S) * lo_step, lo0 + (S) * lo_step + lo_b, desc_hi, idesc, \
+                                           kb > 0 ? 1u : 0u, &empty_bar[S], &full_bar[NS], nphase);                 \
+        if (NS == 0) phase ^= 1;                                                                                    \
+        if (++kb == nkb) {                                                                                          \
+            stage = NS;                                                                                             \
+            break;                                                                                                  \
+        }                                                                                                           \
+    }
+                while (ok && kb < nkb) {
+                    switch (stage) {
+                        case 0: EXFOLD_LP_KBLOCK(0)
+                        case 1: EXFOLD_LP_KBLOCK(1)
+                        case 2: EXFOLD_LP_KBLOCK(2)
+                        case 3: EXFOLD_LP_KBLOCK(3)
+                        case 4: EXFOLD_LP_KBLOCK(4)
+                        default: EXFOLD_LP_KBLOCK(5)
+                    }
+                    if (kb < nkb) stage = 0;  // fell through the last stage: the ring wraps
+                }
+#undef EXFOLD_LP_KBLOCK
+                if (ok) ptx::umma_commit_pair(&tfull_bar[as], 3);
+            }
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------ epilogue warps (own rows; TMEM lane quadrant = warp % 4)
+        const int q = warp & 3, half = (warp - 3) >> 2;
+        float* buf = reinterpret_cast<float*>(tiles + kLpStages * kLpStageBytes + (warp - 3) * kLpOutBytes);
+        const LinearEpilogue<O> ep(p.l);
+        constexpr int kPer = kLpChunk / 4, kRowsAt = 32 / kPer;  // lanes per row, rows per access
+        const int c = lane % kPer * 4, r0 = lane / kPer;
+        int iter = 0;
+        for (int w = w_begin; w < total; w += w_stride, ++iter) {
+            const int as = iter & 1, aphase = (iter >> 1) & 1;
+            int m, n;
+            decode_tile(p, w, &m, &n);
+            const int64_t row0 = (int64_t)m * 256 + rank * kTileM + q * 32;
+            const int rows = (int)max((int64_t)0, min((int64_t)32, p.l.T - row0));
+            const int col0 = n * 256 + half * 128;
+            int ok = 1;
+            if (lane == 0) ok = ptx::mbar_wait_local(&tfull_bar[as], aphase, abort_flag, p.l.status, 4) ? 1 : 0;
+            ok = __shfl_sync(0xffffffffu, ok, 0);
+            if (!ok) break;
+            ptx::tc_fence_after();
+            const uint32_t taddr = tmem_base + as * 256 + half * 128 + ((uint32_t)(q * 32) << 16);
+            if (rows > 0) {
+#pragma unroll 1
+                for (int cc = 0; cc < 128 && col0 + cc < p.l.N; cc += kLpChunk) {
+                    typename LinearEpilogue<O>::Extra extra[kPer];
+                    const int col = col0 + cc + c;
+#pragma unroll
+                    for (int u = 0; u < kPer; ++u)
+                        if (u * kRowsAt + r0 < rows && col < p.l.N) extra[u] = ep.fetch(row0 + u * kRowsAt + r0, col);
+                    uint32_t v[kLpChunk];
+                    tmem_ld16(taddr + cc, v);
+                    ptx::tmem_ld_wait();
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < kPer; ++j)  // 16-byte pieces, swizzled by the row: no bank conflicts either way
+                        *reinterpret_cast<uint4*>(buf + lane * kLpChunk + ((j ^ ((lane >> 1) & (kPer - 1))) << 2)) =
+                            make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                    __syncwarp();
+                    float4 s[kPer];
+#pragma unroll
+                    for (int u = 0; u < kPer; ++u) {
+                        const int r = u * kRowsAt + r0;
+                        s[u] = *reinterpret_cast<const float4*>(buf + r * kLpChunk + (((c >> 2) ^ ((r >> 1) & (kPer - 1))) << 2));
+                    }
+#pragma unroll
+                    for (int u = 0; u < kPer; ++u)
+                        if (u * kRowsAt + r0 < rows && col < p.l.N) ep.finish(row0 + u * kRowsAt + r0, col, s[u], extra[u]);
+                }
+            }
+            ptx::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive_leader(&tempty_bar[as]);
+        }
+    }
+
+    // ------------------------------------------------ teardown
+    if (threadIdx.x == 96) grid_dep_launch();  // after the epilogue loop
+    ptx::tc_fence_before();
+    __syncthreads();
+    if (abort_s) __nanosleep(100000);  // let any copy still in flight land before shared memory is released
+    ptx::cluster_sync_all();           // the peer is done with this CTA's shared and tensor memory
+    if (warp == 2) {
+        ptx::tc_fence_after();
+        ptx::tmem_dealloc_pair(tmem_base, kLpTmemCols);
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_linear_pair(LinearPairParams p, bool out_bf16, int sms, cudaStream_t s) {
+    p.mt = (int)((p.l.T + 255) / 256);
+    p.nt = (p.l.N + 255) / 256;
+    // The row tiles of a band stay in L2 while the weights pass by
+    p.band = (int)std::max<int64_t>(1, std::min<int64_t>(p.mt, (48 << 20) / ((int64_t)p.l.K * 512)));
+    if ((int64_t)p.mt * p.nt > 0x3fffffff) return cudaErrorInvalidValue;
+    const int total = p.mt * p.nt, pairs = std::max(1, sms / 2), rounds = (total + pairs - 1) / pairs;
+    const int grid = 2 * ((total + rounds - 1) / rounds);  // the pairs that take work finish together
+    auto go = [&](auto kernel) {
+        const cudaError_t e = ensure_smem(kernel, kLpSmem);
+        return e != cudaSuccess ? e : launch_pdl_cluster(kernel, grid, kLpThreads, kLpSmem, 2, s, p);
+    };
+    return out_bf16 ? go(linear_pair_kernel<__nv_bfloat16>) : go(linear_pair_kernel<float>);
+}
+
+}  // namespace exfold

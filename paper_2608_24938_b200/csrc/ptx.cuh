@@ -91,6 +91,24 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volati
     }
 }
 
+// Bounded wait that looks at the CTA's own abort flag only: for the first kernel of a call, whose status record may still hold an
+// earlier call's code
+__device__ __forceinline__ bool mbar_wait_local(uint64_t* bar, uint32_t parity, volatile int* abort_flag, DeviceStatus* st, int where) {
+    if (mbar_try_wait(bar, parity)) return true;
+    const uint64_t t0 = globaltimer_ns();
+    for (uint32_t it = 1;; ++it) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((it & 255u) == 0u) {
+            if (*abort_flag) return false;
+            if (globaltimer_ns() - t0 > kWaitLimitNs) {
+                *abort_flag = 1;
+                report_timeout(st, where);
+                return false;
+            }
+        }
+    }
+}
+
 // One lane of a converged warp, the same one each time. The branch of a one-thread issue loop is taken on this and not on
 // lane == 0: the compiler then knows that a single thread runs it and keeps descriptors and addresses in uniform registers
 // (per k-block of four MMAs and a commit 532 -> 355 issue cycles, per stage of three copies 397 -> 275; the pipe needs 512).

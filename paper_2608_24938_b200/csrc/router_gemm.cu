@@ -27,23 +27,6 @@ constexpr int kRThreads = 192;  // warp 0: TMA producer, warp 1: MMA issuer, war
 constexpr int kRMaxStages = 6;
 constexpr int kRBK = 64;
 
-// Bounded wait that looks at the CTA's own abort flag only
-__device__ __forceinline__ bool wait_local(uint64_t* bar, uint32_t parity, volatile int* abort_flag, DeviceStatus* st, int where) {
-    if (ptx::mbar_try_wait(bar, parity)) return true;
-    const uint64_t t0 = ptx::globaltimer_ns();
-    for (uint32_t it = 1;; ++it) {
-        if (ptx::mbar_try_wait(bar, parity)) return true;
-        if ((it & 255u) == 0u) {
-            if (*abort_flag) return false;
-            if (ptx::globaltimer_ns() - t0 > ptx::kWaitLimitNs) {
-                *abort_flag = 1;
-                report_timeout(st, where);
-                return false;
-            }
-        }
-    }
-}
-
 __global__ void __launch_bounds__(kRThreads, 1) router_gemm_kernel(const __grid_constant__ RouterGemmParams p) {
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t full_bar[kRMaxStages];
@@ -86,7 +69,7 @@ __global__ void __launch_bounds__(kRThreads, 1) router_gemm_kernel(const __grid_
         if (ptx::elect_one()) {
             int stage = 0, phase = 0;
             for (int kb = kb0; kb < kb1; ++kb) {
-                if (!wait_local(&empty_bar[stage], phase ^ 1, abort_flag, p.status, 1)) break;
+                if (!ptx::mbar_wait_local(&empty_bar[stage], phase ^ 1, abort_flag, p.status, 1)) break;
                 unsigned char* dst = tiles + stage * stage_bytes;
                 ptx::mbar_expect_tx(&full_bar[stage], stage_bytes);
                 ptx::tma_load_2d(dst, &p.tm_x, &full_bar[stage], kb * kRBK, row0);
@@ -106,7 +89,7 @@ __global__ void __launch_bounds__(kRThreads, 1) router_gemm_kernel(const __grid_
             int stage = 0, phase = 0;
             bool ok = true, ready = false;
             for (int kb = kb0; kb < kb1; ++kb) {
-                if (!ready && !wait_local(&full_bar[stage], phase, abort_flag, p.status, 3)) {
+                if (!ready && !ptx::mbar_wait_local(&full_bar[stage], phase, abort_flag, p.status, 3)) {
                     ok = false;
                     break;
                 }
@@ -124,7 +107,7 @@ __global__ void __launch_bounds__(kRThreads, 1) router_gemm_kernel(const __grid_
         // partial tile -> shared memory (the ring is free once every MMA has completed)
         const int q = warp & 3;
         int ok = 1;
-        if (lane == 0) ok = wait_local(&done_bar, 0, abort_flag, p.status, 4) ? 1 : 0;
+        if (lane == 0) ok = ptx::mbar_wait_local(&done_bar, 0, abort_flag, p.status, 4) ? 1 : 0;
         ok = __shfl_sync(0xffffffffu, ok, 0);
         if (ok) {
             ptx::tc_fence_after();
