@@ -7,6 +7,7 @@ in the CUDA library; there is no fallback: if the library is missing, importing 
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Optional
 
@@ -425,7 +426,7 @@ def make_router(score: str = "softmax", bias: Optional[torch.Tensor] = None, n_g
 
 def _typed(t: Optional[torch.Tensor], dtype, shape) -> Optional[int]:
     if t is not None:
-        assert t.dtype == dtype and tuple(t.shape) == tuple(shape), f"expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}"
+        assert t.dtype == dtype and t.shape == shape, f"expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}"
     return _ptr(t)
 
 
@@ -482,14 +483,20 @@ def exfold_moe_decode_routed(layer, x, ids, w, w_gate, w_up, w_down, tables: exf
 _LINEAR_DTYPES = {torch.float32: EXFOLD_F32, torch.bfloat16: EXFOLD_BF16}
 
 
-def _rows(t: Optional[torch.Tensor], dtype, shape):
-    """Pointer and row distance of a matrix whose rows are contiguous."""
-    if t is None:
-        return None, 0
-    assert t.dtype == dtype and tuple(t.shape) == tuple(shape), f"expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}"
-    assert t.stride(1) == 1 or t.shape[1] == 1, "rows must be contiguous"
-    assert t.stride(0) >= t.shape[1] or t.shape[0] <= 1, "rows must not overlap"
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else 0)
+def _rows(t: torch.Tensor, dtype, rows: int, cols: int) -> int:
+    """Row distance of a matrix whose rows are contiguous (0: of no account)."""
+    assert t.dtype == dtype and t.shape == (rows, cols), f"expected {dtype} {(rows, cols)}, got {t.dtype} {tuple(t.shape)}"
+    ld, step = t.stride()
+    assert step == 1 or cols == 1, "rows must be contiguous"
+    if rows <= 1:
+        return 0
+    assert ld >= cols, "rows must not overlap"
+    return ld
+
+
+@functools.lru_cache(maxsize=1024)
+def _linear_desc(*fields):
+    return C.byref(exfold_linear_desc(*fields))  # by value of its fields; making one costs 2 us of a call
 
 
 def exfold_linear_workspace_bytes(desc: exfold_linear_desc, max_tokens: int) -> int:
@@ -509,13 +516,15 @@ def alloc_linear_workspace(in_features: int, out_features: int, max_tokens: int,
 def exfold_linear(x, w, y, ws, bias=None, residual=None, activation: str = "none", stream=None, check: bool = True) -> int:
     """y = act(x w^T + bias) + residual. x [T][in], w [out][in], bias [out] of one type; y, residual [T][out]. The matrices may
     have any distance between their rows."""
-    T, i, o = x.shape[0], x.shape[1], w.shape[0]
-    xp, ldx = _rows(x, x.dtype, (T, i))
-    wp, ldw = _rows(w, x.dtype, (o, i))
-    yp, ldy = _rows(y, y.dtype, (T, o))
-    rp, ldr = _rows(residual, y.dtype, (T, o))
-    desc = exfold_linear_desc(i, o, _LINEAR_DTYPES[x.dtype], _LINEAR_DTYPES[y.dtype], ACTIVATIONS[activation], ldx, ldw, ldy, ldr)
-    rc = lib.exfold_linear(C.byref(desc), xp, wp, _typed(bias, x.dtype, (o,)), rp, T, yp, _ptr(ws), ws.numel(), _stream(stream))
+    T, i = x.shape
+    o, dt, out = w.shape[0], x.dtype, y.dtype
+    desc = _linear_desc(i, o, _LINEAR_DTYPES[dt], _LINEAR_DTYPES[out], ACTIVATIONS[activation], _rows(x, dt, T, i),
+                        _rows(w, dt, o, i), _rows(y, out, T, o), _rows(residual, out, T, o) if residual is not None else 0)
+    if bias is not None:
+        assert bias.dtype == dt and bias.shape == (o,) and bias.is_contiguous(), f"expected bias {dt} {(o,)}"
+    rc = lib.exfold_linear(desc, x.data_ptr(), w.data_ptr(), bias.data_ptr() if bias is not None else None,
+                           residual.data_ptr() if residual is not None else None, T, y.data_ptr(), ws.data_ptr(), ws.numel(),
+                           _stream(stream))
     if check and rc != 0:
         raise ExfoldError(rc, "exfold_linear")
     return rc

@@ -148,17 +148,18 @@ EncodeTiledFn encode_fn() {
 
 constexpr int kMaxHostChunks = 4;  // host-buffer prefill: chunks of >= 2048 tokens in flight
 
-// bf16 matrix [rows][cols] row-major, rows ld elements apart (0: dense); box = box_rows x kGemmBK columns, 128-byte swizzle (a box row)
-bool make_tmap(CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows, uint64_t ld = 0) {
+// Matrix [rows][cols] row-major, rows ld elements apart (0: dense), of bf16 or fp32; box = box_rows x 128 bytes, 128-byte swizzle (a
+// box row)
+bool make_tmap(CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows, uint64_t ld = 0, bool f32 = false) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
+    const cuuint64_t el = f32 ? 4 : 2;
     cuuint64_t dims[2] = {cols, rows};
-    cuuint64_t strides[1] = {(ld ? ld : cols) * 2};
-    cuuint32_t box[2] = {(cuuint32_t)kGemmBK, box_rows};
+    cuuint64_t strides[1] = {(ld ? ld : cols) * el};
+    cuuint32_t box[2] = {(cuuint32_t)(2 * kGemmBK / el), box_rows};
     cuuint32_t estr[2] = {1, 1};
-    CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
-                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+    CUresult r = fn(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box,
+                    estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS;
 }
@@ -1273,10 +1274,17 @@ int exfold_linear(const exfold_linear_desc* desc, const void* x, const void* w, 
     PdlScope pdl_scope(true);
     if (bf16 && aligned16(x) && aligned16(w) && ((p.ldx | p.ldw) & 7) == 0) {
         const int64_t items = ((T + 255) / 256) * ((p.N + 255) / 256);
-        if (items >= sm_count() / 2) {
+        if (linear_small_fits(p)) {
+            EXFOLD_CUDA(launch_linear_small(p, out_bf16, sm_count(), s));
+        } else if (items >= sm_count() / 2) {
             LinearPairParams q{};
             q.l = p;
             if (!make_tmap(&q.tm_x, x, (uint64_t)T, p.K, 128, p.ldx) || !make_tmap(&q.tm_w, w, (uint64_t)p.N, p.K, 128, p.ldw))
+                return EXFOLD_ERR_CUDA;
+            const int64_t unit = out_bf16 ? 7 : 3;  // rows of whole 16 bytes
+            q.tma_io = aligned16(y) && aligned16(residual) && (p.ldy & unit) == 0 && (residual == nullptr || (p.ldr & unit) == 0);
+            if (q.tma_io && (!make_tmap(&q.tm_y, y, (uint64_t)T, p.N, 32, p.ldy, !out_bf16) ||
+                             (residual && !make_tmap(&q.tm_r, residual, (uint64_t)T, p.N, 32, p.ldr, !out_bf16))))
                 return EXFOLD_ERR_CUDA;
             EXFOLD_CUDA(launch_linear_pair(q, out_bf16, sm_count(), s));
         } else {

@@ -483,6 +483,9 @@ struct LinearParams {
     DeviceStatus* status;  // cleared by the call's first kernel
 };
 cudaError_t launch_linear_simt(const LinearParams& p, bool bf16, bool out_bf16, int sms, cudaStream_t s);
+// bf16, at most 8 tokens (linear_small.cu)
+bool linear_small_fits(const LinearParams& p);
+cudaError_t launch_linear_small(const LinearParams& p, bool out_bf16, int sms, cudaStream_t s);
 // bf16 on the tensor cores, K split over a cluster (linear_tile.cu)
 struct LinearTilePlan {
     int a_rows, bn, split, stages;  // token rows and features per tile, CTAs per tile, ring
@@ -501,7 +504,10 @@ struct LinearPairParams {
     LinearParams l;
     CUtensorMap tm_x;  // box 128 x 64
     CUtensorMap tm_w;  // box 128 x 64
-    int mt, nt, band;  // tiles; row tiles that share a weight tile in a run of the work order
+    CUtensorMap tm_y;  // tma_io: y and the residual, boxes of 32 rows x 128 bytes
+    CUtensorMap tm_r;
+    int tma_io;
+    int mt, nt, band;  // set by the launcher: tiles; row tiles that share a weight tile in a run of the work order
 };
 cudaError_t launch_linear_pair(LinearPairParams p, bool out_bf16, int sms, cudaStream_t s);
 

@@ -4,8 +4,11 @@
 // 128 x 256 tile needs 48 KB for the same. Six stages of 32 KB are in flight, two 256-column accumulators hand a finished tile to the
 // epilogue warps while the next one is multiplied. Roles per CTA: warps 0 and 1 TMA producers (k-blocks dealt in turn; own token
 // rows, own half of the weight rows, both CTAs' bytes counted on the leader's barrier), warp 2 MMA issuer (leader), the other eight
-// epilogue: two per quadrant of the accumulator's lanes, half of the columns each. An epilogue warp passes 32 columns at a time
-// through shared memory so that residual and result move in whole rows of 64 or 128 bytes.
+// epilogue: two per quadrant of the accumulator's lanes, half of the columns each.
+//
+// An epilogue warp works on 32 rows x 128 bytes of y at a time: the residual comes into its buffer by TMA, each lane adds its row of
+// the accumulator in place, and the buffer leaves by TMA, which also clips what lies past T and N. Where y or the residual is not
+// aligned for that, rows go through shared memory and plain loads and stores.
 #include <algorithm>
 
 #include "common.cuh"
@@ -21,8 +24,8 @@ constexpr int kLpStages = 6;
 constexpr int kLpTileBytes = kTileM * kLpBK * 2;  // 16 KB: this CTA's token rows, or its half of the weight rows
 constexpr int kLpStageBytes = 2 * kLpTileBytes;
 constexpr int kLpEpiWarps = 8;
-constexpr int kLpChunk = 16;                           // accumulator columns per trip through shared memory
-constexpr int kLpOutBytes = 32 * kLpChunk * 4;         // per epilogue warp
+constexpr int kLpOutBytes = 32 * 128;                  // per epilogue warp: 32 rows x 128 bytes
+constexpr int kLpChunk = 16;                           // unaligned y: accumulator columns per trip through it
 constexpr int kLpSmem = kLpStages * kLpStageBytes + kLpEpiWarps * kLpOutBytes + 1024;
 constexpr int kLpThreads = 32 * (3 + kLpEpiWarps);
 constexpr int kLpTmemCols = 512;
@@ -45,13 +48,57 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
         : "memory");
 }
 
-template <typename O>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<uint32_t*>(&v);
+}
+
+// 32 accumulator columns from `col` on: bias and activation. FULL: all 32 exist and the bias is aligned to 16 bytes.
+template <int ACT, bool FULL>
+__device__ __forceinline__ void bias_act(float (&f)[32], const uint32_t (&v)[32], const LinearParams& l, int col) {
+    const __nv_bfloat16* bias = reinterpret_cast<const __nv_bfloat16*>(l.bias) + col;
+    if (l.bias == nullptr) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]);
+    } else if (FULL) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {  // every lane the same address
+            const uint4 b = __ldg(reinterpret_cast<const uint4*>(bias) + j);
+            const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&b);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float2 t = __bfloat1622float2(h[u]);
+                f[8 * j + 2 * u] = __uint_as_float(v[8 * j + 2 * u]) + t.x;
+                f[8 * j + 2 * u + 1] = __uint_as_float(v[8 * j + 2 * u + 1]) + t.y;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]) + (col + j < l.N ? __bfloat162float(bias[j]) : 0.f);
+    }
+#pragma unroll
+    for (int j = 0; j < 32; ++j) f[j] = linear_act(f[j], ACT);
+}
+template <bool FULL>
+__device__ __forceinline__ void bias_act(float (&f)[32], const uint32_t (&v)[32], const LinearParams& l, int col) {
+    switch (l.act) {
+        case EXFOLD_ACT_RELU: return bias_act<EXFOLD_ACT_RELU, FULL>(f, v, l, col);
+        case EXFOLD_ACT_GELU: return bias_act<EXFOLD_ACT_GELU, FULL>(f, v, l, col);
+        case EXFOLD_ACT_GELU_TANH: return bias_act<EXFOLD_ACT_GELU_TANH, FULL>(f, v, l, col);
+        case EXFOLD_ACT_SILU: return bias_act<EXFOLD_ACT_SILU, FULL>(f, v, l, col);
+        default: return bias_act<EXFOLD_ACT_NONE, FULL>(f, v, l, col);
+    }
+}
+
+// TMA: y and the residual go by tensor maps
+template <typename O, bool TMA>
 __global__ void __launch_bounds__(kLpThreads, 1) linear_pair_kernel(const __grid_constant__ LinearPairParams p) {
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t full_bar[kLpStages];   // used in the leader
     __shared__ __align__(8) uint64_t empty_bar[kLpStages];  // one per CTA, released by the leader's commits
     __shared__ __align__(8) uint64_t tfull_bar[2];          // one per CTA
     __shared__ __align__(8) uint64_t tempty_bar[2];         // used in the leader: the epilogue warps of both CTAs
+    __shared__ __align__(8) uint64_t res_bar[kLpEpiWarps];  // an epilogue warp's residual
     __shared__ uint32_t tmem_base_s;
     __shared__ int abort_s;
     unsigned char* tiles =
@@ -69,6 +116,9 @@ __global__ void __launch_bounds__(kLpThreads, 1) linear_pair_kernel(const __grid
             ptx::mbar_init(&tfull_bar[s], 1);
             ptx::mbar_init(&tempty_bar[s], 2 * kLpEpiWarps);
         }
+        for (int s = 0; s < kLpEpiWarps; ++s) ptx::mbar_init(&res_bar[s], 1);
+        if (TMA) ptx::prefetch_tmap(&p.tm_y);
+        if (TMA && p.l.residual != nullptr) ptx::prefetch_tmap(&p.tm_r);
         abort_s = 0;
         ptx::fence_mbar_init();
     }
@@ -169,10 +219,11 @@ __global__ void __launch_bounds__(kLpThreads, 1) linear_pair_kernel(const __grid
     } else {
         // ------------------------------------------------ epilogue warps (own rows; TMEM lane quadrant = warp % 4)
         const int q = warp & 3, half = (warp - 3) >> 2;
-        float* buf = reinterpret_cast<float*>(tiles + kLpStages * kLpStageBytes + (warp - 3) * kLpOutBytes);
-        const LinearEpilogue<O> ep(p.l);
-        constexpr int kPer = kLpChunk / 4, kRowsAt = 32 / kPer;  // lanes per row, rows per access
-        const int c = lane % kPer * 4, r0 = lane / kPer;
+        unsigned char* buf = tiles + kLpStages * kLpStageBytes + (warp - 3) * kLpOutBytes;
+        uint64_t* rbar = &res_bar[warp - 3];
+        const bool has_res = p.l.residual != nullptr, full_bias = (reinterpret_cast<uintptr_t>(p.l.bias) & 15) == 0;
+        constexpr int kCols = 128 / (int)sizeof(O);  // of y per trip
+        uint32_t rphase = 0;
         int iter = 0;
         for (int w = w_begin; w < total; w += w_stride, ++iter) {
             const int as = iter & 1, aphase = (iter >> 1) & 1;
@@ -182,12 +233,78 @@ __global__ void __launch_bounds__(kLpThreads, 1) linear_pair_kernel(const __grid
             const int rows = (int)max((int64_t)0, min((int64_t)32, p.l.T - row0));
             const int col0 = n * 256 + half * 128;
             int ok = 1;
+            const bool some = rows > 0 && col0 < p.l.N;
+            if (TMA && some && has_res && lane == 0) {  // on its way while the tile is multiplied
+                ptx::tma_store_wait_read();
+                ptx::mbar_expect_tx(rbar, kLpOutBytes);
+                ptx::tma_load_2d(buf, &p.tm_r, rbar, col0, (int)row0);
+            }
             if (lane == 0) ok = ptx::mbar_wait_local(&tfull_bar[as], aphase, abort_flag, p.l.status, 4) ? 1 : 0;
             ok = __shfl_sync(0xffffffffu, ok, 0);
             if (!ok) break;
             ptx::tc_fence_after();
             const uint32_t taddr = tmem_base + as * 256 + half * 128 + ((uint32_t)(q * 32) << 16);
-            if (rows > 0) {
+            if (TMA && some) {
+#pragma unroll 1
+                for (int cc = 0; cc < 128 && col0 + cc < p.l.N; cc += kCols) {
+                    if (has_res) {  // every lane sees the copy's end itself, and with it the bytes
+                        ok = ptx::mbar_wait_local(rbar, rphase, abort_flag, p.l.status, 5) ? 1 : 0;
+                        rphase ^= 1;
+                        ok = __all_sync(0xffffffffu, ok);
+                    } else {
+                        if (lane == 0) ptx::tma_store_wait_read();  // the buffer is free
+                        __syncwarp();
+                    }
+                    if (!ok) break;
+#pragma unroll
+                    for (int h = 0; h < kCols / 32; ++h) {
+                        const int col = col0 + cc + 32 * h;
+                        uint32_t v[32];
+                        float f[32];
+                        ptx::tmem_ld32(taddr + cc + 32 * h, v);
+                        ptx::tmem_ld_wait();
+                        if (full_bias && col + 32 <= p.l.N) bias_act<true>(f, v, p.l, col);
+                        else bias_act<false>(f, v, p.l, col);
+                        constexpr int kPieces = 32 * (int)sizeof(O) / 16;  // of 16 bytes; chunk c of a row lies at c ^ (row & 7)
+#pragma unroll
+                        for (int j = 0; j < kPieces; ++j) {
+                            uint4* at = reinterpret_cast<uint4*>(buf + lane * 128 + (((h * kPieces + j) ^ (lane & 7)) << 4));
+                            uint4 o = has_res ? *at : make_uint4(0u, 0u, 0u, 0u);
+                            if constexpr (sizeof(O) == 2) {
+                                const __nv_bfloat162* r = reinterpret_cast<const __nv_bfloat162*>(&o);
+                                float g[8];
+#pragma unroll
+                                for (int u = 0; u < 4; ++u) {
+                                    const float2 t = __bfloat1622float2(r[u]);
+                                    g[2 * u] = has_res ? f[8 * j + 2 * u] + t.x : f[8 * j + 2 * u];
+                                    g[2 * u + 1] = has_res ? f[8 * j + 2 * u + 1] + t.y : f[8 * j + 2 * u + 1];
+                                }
+                                o = make_uint4(pack2(g[0], g[1]), pack2(g[2], g[3]), pack2(g[4], g[5]), pack2(g[6], g[7]));
+                            } else {
+                                float* g = reinterpret_cast<float*>(&o);
+#pragma unroll
+                                for (int u = 0; u < 4; ++u) g[u] = has_res ? f[4 * j + u] + g[u] : f[4 * j + u];
+                            }
+                            *at = o;
+                        }
+                    }
+                    ptx::store_fence();
+                    __syncwarp();
+                    if (lane == 0) {
+                        ptx::tma_store_2d(&p.tm_y, buf, col0 + cc, (int)row0);
+                        if (has_res && cc + kCols < 128 && col0 + cc + kCols < p.l.N) {  // the next columns' residual
+                            ptx::tma_store_wait_read();
+                            ptx::mbar_expect_tx(rbar, kLpOutBytes);
+                            ptx::tma_load_2d(buf, &p.tm_r, rbar, col0 + cc + kCols, (int)row0);
+                        }
+                    }
+                }
+                if (!ok) break;
+            } else if (!TMA && some) {
+                const LinearEpilogue<O> ep(p.l);
+                float* fbuf = reinterpret_cast<float*>(buf);
+                constexpr int kPer = kLpChunk / 4, kRowsAt = 32 / kPer;  // lanes per row, rows per access
+                const int c = lane % kPer * 4, r0 = lane / kPer;
 #pragma unroll 1
                 for (int cc = 0; cc < 128 && col0 + cc < p.l.N; cc += kLpChunk) {
                     typename LinearEpilogue<O>::Extra extra[kPer];
@@ -201,14 +318,14 @@ __global__ void __launch_bounds__(kLpThreads, 1) linear_pair_kernel(const __grid
                     __syncwarp();
 #pragma unroll
                     for (int j = 0; j < kPer; ++j)  // 16-byte pieces, swizzled by the row: no bank conflicts either way
-                        *reinterpret_cast<uint4*>(buf + lane * kLpChunk + ((j ^ ((lane >> 1) & (kPer - 1))) << 2)) =
+                        *reinterpret_cast<uint4*>(fbuf + lane * kLpChunk + ((j ^ ((lane >> 1) & (kPer - 1))) << 2)) =
                             make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
                     __syncwarp();
                     float4 s[kPer];
 #pragma unroll
                     for (int u = 0; u < kPer; ++u) {
                         const int r = u * kRowsAt + r0;
-                        s[u] = *reinterpret_cast<const float4*>(buf + r * kLpChunk + (((c >> 2) ^ ((r >> 1) & (kPer - 1))) << 2));
+                        s[u] = *reinterpret_cast<const float4*>(fbuf + r * kLpChunk + (((c >> 2) ^ ((r >> 1) & (kPer - 1))) << 2));
                     }
 #pragma unroll
                     for (int u = 0; u < kPer; ++u)
@@ -219,6 +336,7 @@ __global__ void __launch_bounds__(kLpThreads, 1) linear_pair_kernel(const __grid
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive_leader(&tempty_bar[as]);
         }
+        if (TMA && lane == 0) ptx::tma_store_wait();
     }
 
     // ------------------------------------------------ teardown
@@ -247,7 +365,8 @@ cudaError_t launch_linear_pair(LinearPairParams p, bool out_bf16, int sms, cudaS
         const cudaError_t e = ensure_smem(kernel, kLpSmem);
         return e != cudaSuccess ? e : launch_pdl_cluster(kernel, grid, kLpThreads, kLpSmem, 2, s, p);
     };
-    return out_bf16 ? go(linear_pair_kernel<__nv_bfloat16>) : go(linear_pair_kernel<float>);
+    if (out_bf16) return p.tma_io ? go(linear_pair_kernel<__nv_bfloat16, true>) : go(linear_pair_kernel<__nv_bfloat16, false>);
+    return p.tma_io ? go(linear_pair_kernel<float, true>) : go(linear_pair_kernel<float, false>);
 }
 
 }  // namespace exfold
