@@ -1273,10 +1273,9 @@ int exfold_linear(const exfold_linear_desc* desc, const void* x, const void* w, 
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
     PdlScope pdl_scope(true);
     if (bf16 && aligned16(x) && aligned16(w) && ((p.ldx | p.ldw) & 7) == 0) {
-        const int64_t items = ((T + 255) / 256) * ((p.N + 255) / 256);
         if (linear_small_fits(p)) {
             EXFOLD_CUDA(launch_linear_small(p, out_bf16, sm_count(), s));
-        } else if (items >= sm_count() / 2) {
+        } else if (linear_prefers_pairs(T, p.N, p.K, sm_count())) {
             LinearPairParams q{};
             q.l = p;
             if (!make_tmap(&q.tm_x, x, (uint64_t)T, p.K, 128, p.ldx) || !make_tmap(&q.tm_w, w, (uint64_t)p.N, p.K, 128, p.ldw))

@@ -492,6 +492,7 @@ struct LinearTilePlan {
     size_t smem;
 };
 LinearTilePlan linear_tile_plan(int64_t T, int N, int K, int sms);
+bool linear_prefers_pairs(int64_t T, int N, int K, int sms);
 struct LinearTileParams {
     LinearParams l;
     CUtensorMap tm_x;  // x, box a_rows x 64

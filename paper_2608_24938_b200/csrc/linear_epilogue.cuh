@@ -1,5 +1,7 @@
 // What the dense-product kernels do to their sums: bias, activation, residual, one rounding to the output type.
 #pragma once
+#include <cooperative_groups.h>
+
 #include "common.cuh"
 
 namespace exfold {
@@ -32,55 +34,168 @@ __device__ __forceinline__ void linear_store4(__nv_bfloat16* p, const float4& v)
     *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(h);
 }
 
-// Four neighbouring outputs (n a multiple of 4) of a row, bf16 operands; O is y's and the residual's type. Rows that are not
-// aligned to four elements, and the last N % 4 columns, go element by element.
+template <typename O>
+struct LinearFour;  // four neighbours as they lie in memory
+template <>
+struct LinearFour<float> { using type = float4; };
+template <>
+struct LinearFour<__nv_bfloat16> { using type = uint2; };
+
+// Four neighbouring outputs of a row, bf16 operands; O is y's and the residual's type. For products whose groups of four are all whole
+// and aligned (whole()).
 template <typename O>
 struct LinearEpilogue {
+    using Raw = typename LinearFour<O>::type;
     const LinearParams& p;
-    const bool vec;       // y and residual
-    const bool vec_bias;
-    __device__ __forceinline__ explicit LinearEpilogue(const LinearParams& q)
-        : p(q),
-          vec(((reinterpret_cast<uintptr_t>(q.y) | reinterpret_cast<uintptr_t>(q.residual)) & (4 * sizeof(O) - 1)) == 0 &&
-              (q.ldy & 3) == 0 && (q.residual == nullptr || (q.ldr & 3) == 0)),
-          vec_bias((reinterpret_cast<uintptr_t>(q.bias) & 7) == 0) {}
+    __host__ __device__ __forceinline__ explicit LinearEpilogue(const LinearParams& q) : p(q) {}
+    __host__ __device__ __forceinline__ bool whole() const {
+        const uintptr_t rows = reinterpret_cast<uintptr_t>(p.y) | reinterpret_cast<uintptr_t>(p.residual);
+        return (rows & (4 * sizeof(O) - 1)) == 0 && (reinterpret_cast<uintptr_t>(p.bias) & 7) == 0 &&
+               ((p.ldy | p.N | (p.residual != nullptr ? p.ldr : 0)) & 3) == 0;
+    }
+    // What comes from memory, asked for before the sum is there. Kept as it was loaded: a conversion would wait for the load, and
+    // the next loads for the conversion.
     struct Extra {
-        float4 bias, residual;
+        uint2 bias;
+        Raw residual;
     };
-    // What comes from memory, asked for before the sum is there
     __device__ __forceinline__ Extra fetch(int64_t m, int n) const {
         Extra e;
-        e.bias = e.residual = make_float4(0.f, 0.f, 0.f, 0.f);
-        const bool four = n + 4 <= p.N;
-        if (p.bias != nullptr) {
-            const __nv_bfloat16* b = reinterpret_cast<const __nv_bfloat16*>(p.bias) + n;
-            if (vec_bias && four) e.bias = linear_load4(b);
-            else each(n, [&](int j) { at(e.bias, j) = linear_f32(b[j]); });
-        }
-        if (p.residual != nullptr) {
-            const O* r = reinterpret_cast<const O*>(p.residual) + m * p.ldr + n;
-            if (vec && four) e.residual = linear_load4(r);
-            else each(n, [&](int j) { at(e.residual, j) = linear_f32(r[j]); });
-        }
+        e.bias = make_uint2(0u, 0u);
+        e.residual = Raw{};
+        if (p.bias != nullptr) e.bias = *reinterpret_cast<const uint2*>(reinterpret_cast<const __nv_bfloat16*>(p.bias) + n);
+        if (p.residual != nullptr) e.residual = *reinterpret_cast<const Raw*>(reinterpret_cast<const O*>(p.residual) + m * p.ldr + n);
         return e;
     }
     __device__ __forceinline__ void finish(int64_t m, int n, float4 s, const Extra& e) const {
-        s.x = linear_act(s.x + e.bias.x, p.act) + e.residual.x;
-        s.y = linear_act(s.y + e.bias.y, p.act) + e.residual.y;
-        s.z = linear_act(s.z + e.bias.z, p.act) + e.residual.z;
-        s.w = linear_act(s.w + e.bias.w, p.act) + e.residual.w;
-        O* y = reinterpret_cast<O*>(p.y) + m * p.ldy + n;
-        if (vec && n + 4 <= p.N) linear_store4(y, s);
-        else each(n, [&](int j) { linear_store(y + j, at(s, j)); });
+        if (p.bias != nullptr) {
+            const float4 b = linear_load4(reinterpret_cast<const __nv_bfloat16*>(&e.bias));
+            s = make_float4(s.x + b.x, s.y + b.y, s.z + b.z, s.w + b.w);
+        }
+        s = make_float4(linear_act(s.x, p.act), linear_act(s.y, p.act), linear_act(s.z, p.act), linear_act(s.w, p.act));
+        if (p.residual != nullptr) {
+            const float4 r = linear_load4(reinterpret_cast<const O*>(&e.residual));
+            s = make_float4(s.x + r.x, s.y + r.y, s.z + r.z, s.w + r.w);
+        }
+        linear_store4(reinterpret_cast<O*>(p.y) + m * p.ldy + n, s);
     }
+};
 
-private:
-    static __device__ __forceinline__ float& at(float4& v, int j) { return j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w; }
-    template <typename F>
-    __device__ __forceinline__ void each(int n, const F& f) const {
+// The S partial tiles of a cluster (rows x cols floats, cols 32, 64, 128 or 256, rows `ld` floats apart, at `part` in the shared memory of
+// the cluster's CTAs first + k step) added up in the order of k and taken through the epilogue. The CTAs share the work: this one is
+// number `me` of S, and its thread `tid` of THREADS takes every so-manieth group of four outputs. Bias and residual of U groups are
+// asked for ahead, the first ones by begin(), while the products are still running; all loads of U groups are in flight together
+// (those of places past the tile's end go to its last place). In a chain they made this part of a 128 x 256 tile 20 us.
+// WHOLE: every group of four outputs is whole and aligned; else a thread takes single outputs, neighbours in neighbouring lanes.
+template <int S, typename O, int THREADS, bool WHOLE>
+struct LinearReduce {
+    static constexpr int U = S >= 8 ? 1 : S == 1 ? 4 : 2, kStride = S * THREADS;
+    const LinearEpilogue<O>& ep;
+    int rows, shift, total, n0, i0;
+    int64_t row0;
+    typename LinearEpilogue<O>::Extra extra[U];
+
+    __device__ __forceinline__ LinearReduce(const LinearEpilogue<O>& e, int rows_, int cols, int64_t row0_, int n0_, int me, int tid)
+        : ep(e), rows(rows_), shift(cols == 256 ? 6 : cols == 128 ? 5 : cols == 64 ? 4 : 3), total(rows_ << shift), n0(n0_), i0(me * THREADS + tid), row0(row0_) {}
+    __device__ __forceinline__ void begin() {
+        if (i0 >= total) return;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (n + j < p.N) f(j);
+        for (int u = 0; u < U; ++u) {
+            const int i = min(i0 + u * kStride, total - 1), r = i >> shift, c = (i - (r << shift)) * 4;
+            extra[u] = ep.fetch(row0 + r, min(n0 + c, ep.p.N - 4));
+        }
+    }
+    __device__ __forceinline__ void run(const float* part, int ld, int first, int step) {
+        cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+        const float* src[S];
+#pragma unroll
+        for (int k = 0; k < S; ++k) src[k] = S == 1 ? part : cluster.map_shared_rank(const_cast<float*>(part), first + k * step);
+        for (; i0 < total; i0 += U * kStride) {
+            float4 v[U][S];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = min(i0 + u * kStride, total - 1), r = i >> shift, c = (i - (r << shift)) * 4;
+#pragma unroll
+                for (int k = 0; k < S; ++k) v[u][k] = *reinterpret_cast<const float4*>(src[k] + (size_t)r * ld + c);
+            }
+            typename LinearEpilogue<O>::Extra now[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) now[u] = extra[u];
+            const int at = i0;
+            i0 += U * kStride;
+            begin();
+            i0 = at;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = i0 + u * kStride, r = i >> shift, c = (i - (r << shift)) * 4;
+                float4 t = v[u][0];
+#pragma unroll
+                for (int k = 1; k < S; ++k) {
+                    t.x += v[u][k].x;
+                    t.y += v[u][k].y;
+                    t.z += v[u][k].z;
+                    t.w += v[u][k].w;
+                }
+                if (i < total && n0 + c < ep.p.N) ep.finish(row0 + r, n0 + c, t, now[u]);
+            }
+        }
+    }
+};
+template <int S, typename O, int THREADS>
+struct LinearReduce<S, O, THREADS, false> {
+    static constexpr int U = S >= 8 ? 2 : S == 4 ? 4 : 8, kStride = S * THREADS;
+    const LinearParams& l;
+    int shift, total, n0, i0;
+    int64_t row0;
+    __nv_bfloat16 bias[U];
+    O residual[U];
+
+    __device__ __forceinline__ LinearReduce(const LinearEpilogue<O>& e, int rows, int cols, int64_t row0_, int n0_, int me, int tid)
+        : l(e.p), shift(cols == 256 ? 8 : cols == 128 ? 7 : cols == 64 ? 6 : 5), total(rows << shift), n0(n0_), i0(me * THREADS + tid), row0(row0_) {}
+    __device__ __forceinline__ void begin() {
+        if (i0 >= total) return;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = min(i0 + u * kStride, total - 1), r = i >> shift, n = min(n0 + i - (r << shift), l.N - 1);
+            if (l.bias != nullptr) bias[u] = reinterpret_cast<const __nv_bfloat16*>(l.bias)[n];
+            if (l.residual != nullptr) residual[u] = reinterpret_cast<const O*>(l.residual)[(row0 + r) * l.ldr + n];
+        }
+    }
+    __device__ __forceinline__ void run(const float* part, int ld, int first, int step) {
+        cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+        const float* src[S];
+#pragma unroll
+        for (int k = 0; k < S; ++k) src[k] = S == 1 ? part : cluster.map_shared_rank(const_cast<float*>(part), first + k * step);
+        for (; i0 < total; i0 += U * kStride) {
+            float v[U][S];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = min(i0 + u * kStride, total - 1), r = i >> shift;
+#pragma unroll
+                for (int k = 0; k < S; ++k) v[u][k] = src[k][(size_t)r * ld + i - (r << shift)];
+            }
+            float b[U], a[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                b[u] = l.bias != nullptr ? linear_f32(bias[u]) : 0.f;
+                a[u] = l.residual != nullptr ? linear_f32(residual[u]) : 0.f;
+            }
+            const int at = i0;
+            i0 += U * kStride;
+            begin();
+            i0 = at;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = i0 + u * kStride, r = i >> shift, n = n0 + i - (r << shift);
+                float t = v[u][0];
+#pragma unroll
+                for (int k = 1; k < S; ++k) t += v[u][k];
+                if (l.bias != nullptr) t += b[u];
+                t = linear_act(t, l.act);
+                if (l.residual != nullptr) t += a[u];
+                if (i < total && n < l.N) linear_store(reinterpret_cast<O*>(l.y) + (row0 + r) * l.ldy + n, t);
+            }
+        }
     }
 };
 

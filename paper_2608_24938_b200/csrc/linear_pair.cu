@@ -8,7 +8,7 @@
 //
 // An epilogue warp works on 32 rows x 128 bytes of y at a time: the residual comes into its buffer by TMA, each lane adds its row of
 // the accumulator in place, and the buffer leaves by TMA, which also clips what lies past T and N. Where y or the residual is not
-// aligned for that, rows go through shared memory and plain loads and stores.
+// aligned for that, rows go through the buffer and plain loads and stores.
 #include <algorithm>
 
 #include "common.cuh"
@@ -24,8 +24,7 @@ constexpr int kLpStages = 6;
 constexpr int kLpTileBytes = kTileM * kLpBK * 2;  // 16 KB: this CTA's token rows, or its half of the weight rows
 constexpr int kLpStageBytes = 2 * kLpTileBytes;
 constexpr int kLpEpiWarps = 8;
-constexpr int kLpOutBytes = 32 * 128;                  // per epilogue warp: 32 rows x 128 bytes
-constexpr int kLpChunk = 16;                           // unaligned y: accumulator columns per trip through it
+constexpr int kLpOutBytes = 32 * 128;             // per epilogue warp: 32 rows x 128 bytes
 constexpr int kLpSmem = kLpStages * kLpStageBytes + kLpEpiWarps * kLpOutBytes + 1024;
 constexpr int kLpThreads = 32 * (3 + kLpEpiWarps);
 constexpr int kLpTmemCols = 512;
@@ -36,16 +35,6 @@ __device__ __forceinline__ void decode_tile(const LinearPairParams& p, int w, in
     const int rows = min(p.band, p.mt - b * p.band);
     *n = left / rows;
     *m = b * p.band + left - *n * rows;
-}
-
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(taddr)
-        : "memory");
 }
 
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
@@ -88,6 +77,56 @@ __device__ __forceinline__ void bias_act(float (&f)[32], const uint32_t (&v)[32]
         case EXFOLD_ACT_SILU: return bias_act<EXFOLD_ACT_SILU, FULL>(f, v, l, col);
         default: return bias_act<EXFOLD_ACT_NONE, FULL>(f, v, l, col);
     }
+}
+
+// 32 columns (the h-th of the warp's buffer) of this lane's row, onto the residual that lies there or in place of nothing. 16-byte
+// chunk c of a row lies at c ^ (row & 7), the tensor maps' swizzle.
+template <typename O>
+__device__ __forceinline__ void put_cols(unsigned char* buf, int lane, int h, const float (&f)[32], bool has_res) {
+    constexpr int kPieces = 32 * (int)sizeof(O) / 16;
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+        uint4* at = reinterpret_cast<uint4*>(buf + lane * 128 + (((h * kPieces + j) ^ (lane & 7)) << 4));
+        uint4 o = has_res ? *at : make_uint4(0u, 0u, 0u, 0u);
+        if constexpr (sizeof(O) == 2) {
+            const __nv_bfloat162* r = reinterpret_cast<const __nv_bfloat162*>(&o);
+            float g[8];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float2 t = __bfloat1622float2(r[u]);
+                g[2 * u] = has_res ? f[8 * j + 2 * u] + t.x : f[8 * j + 2 * u];
+                g[2 * u + 1] = has_res ? f[8 * j + 2 * u + 1] + t.y : f[8 * j + 2 * u + 1];
+            }
+            o = make_uint4(pack2(g[0], g[1]), pack2(g[2], g[3]), pack2(g[4], g[5]), pack2(g[6], g[7]));
+        } else {
+            float* g = reinterpret_cast<float*>(&o);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) g[u] = has_res ? f[4 * j + u] + g[u] : f[4 * j + u];
+        }
+        *at = o;
+    }
+}
+// The warp's 32 rows x 32 sums to memory, for y or a residual that no tensor map takes: through the buffer, so that a row's 32
+// columns are loaded and stored at once
+template <typename O>
+__device__ __forceinline__ void store_rows(const LinearParams& l, unsigned char* buf, int lane, const float (&f)[32], int64_t row0, int rows,
+                                           int col) {
+    put_cols<float>(buf, lane, 0, f, false);
+    __syncwarp();
+    const bool in = col + lane < l.N;
+    O* y = reinterpret_cast<O*>(l.y) + row0 * l.ldy + col + lane;
+    const O* r = reinterpret_cast<const O*>(l.residual) + row0 * l.ldr + col + lane;
+    for (int i0 = 0; i0 < rows; i0 += 8) {
+        float add[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) add[i] = l.residual != nullptr && in && i0 + i < rows ? linear_f32(r[(i0 + i) * l.ldr]) : 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float v = *reinterpret_cast<const float*>(buf + (i0 + i) * 128 + (((lane >> 2) ^ (i & 7)) << 4) + (lane & 3) * 4);
+            if (in && i0 + i < rows) linear_store(y + (i0 + i) * l.ldy, l.residual != nullptr ? v + add[i] : v);
+        }
+    }
+    __syncwarp();
 }
 
 // TMA: y and the residual go by tensor maps
@@ -265,28 +304,7 @@ __global__ void __launch_bounds__(kLpThreads, 1) linear_pair_kernel(const __grid
                         ptx::tmem_ld_wait();
                         if (full_bias && col + 32 <= p.l.N) bias_act<true>(f, v, p.l, col);
                         else bias_act<false>(f, v, p.l, col);
-                        constexpr int kPieces = 32 * (int)sizeof(O) / 16;  // of 16 bytes; chunk c of a row lies at c ^ (row & 7)
-#pragma unroll
-                        for (int j = 0; j < kPieces; ++j) {
-                            uint4* at = reinterpret_cast<uint4*>(buf + lane * 128 + (((h * kPieces + j) ^ (lane & 7)) << 4));
-                            uint4 o = has_res ? *at : make_uint4(0u, 0u, 0u, 0u);
-                            if constexpr (sizeof(O) == 2) {
-                                const __nv_bfloat162* r = reinterpret_cast<const __nv_bfloat162*>(&o);
-                                float g[8];
-#pragma unroll
-                                for (int u = 0; u < 4; ++u) {
-                                    const float2 t = __bfloat1622float2(r[u]);
-                                    g[2 * u] = has_res ? f[8 * j + 2 * u] + t.x : f[8 * j + 2 * u];
-                                    g[2 * u + 1] = has_res ? f[8 * j + 2 * u + 1] + t.y : f[8 * j + 2 * u + 1];
-                                }
-                                o = make_uint4(pack2(g[0], g[1]), pack2(g[2], g[3]), pack2(g[4], g[5]), pack2(g[6], g[7]));
-                            } else {
-                                float* g = reinterpret_cast<float*>(&o);
-#pragma unroll
-                                for (int u = 0; u < 4; ++u) g[u] = has_res ? f[4 * j + u] + g[u] : f[4 * j + u];
-                            }
-                            *at = o;
-                        }
+                        put_cols<O>(buf, lane, h, f, has_res);
                     }
                     ptx::store_fence();
                     __syncwarp();
@@ -301,35 +319,15 @@ __global__ void __launch_bounds__(kLpThreads, 1) linear_pair_kernel(const __grid
                 }
                 if (!ok) break;
             } else if (!TMA && some) {
-                const LinearEpilogue<O> ep(p.l);
-                float* fbuf = reinterpret_cast<float*>(buf);
-                constexpr int kPer = kLpChunk / 4, kRowsAt = 32 / kPer;  // lanes per row, rows per access
-                const int c = lane % kPer * 4, r0 = lane / kPer;
 #pragma unroll 1
-                for (int cc = 0; cc < 128 && col0 + cc < p.l.N; cc += kLpChunk) {
-                    typename LinearEpilogue<O>::Extra extra[kPer];
-                    const int col = col0 + cc + c;
-#pragma unroll
-                    for (int u = 0; u < kPer; ++u)
-                        if (u * kRowsAt + r0 < rows && col < p.l.N) extra[u] = ep.fetch(row0 + u * kRowsAt + r0, col);
-                    uint32_t v[kLpChunk];
-                    tmem_ld16(taddr + cc, v);
+                for (int col = col0; col < min(col0 + 128, p.l.N); col += 32) {
+                    uint32_t v[32];
+                    float f[32];
+                    ptx::tmem_ld32(taddr + col - col0, v);
                     ptx::tmem_ld_wait();
-                    __syncwarp();
-#pragma unroll
-                    for (int j = 0; j < kPer; ++j)  // 16-byte pieces, swizzled by the row: no bank conflicts either way
-                        *reinterpret_cast<uint4*>(fbuf + lane * kLpChunk + ((j ^ ((lane >> 1) & (kPer - 1))) << 2)) =
-                            make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-                    __syncwarp();
-                    float4 s[kPer];
-#pragma unroll
-                    for (int u = 0; u < kPer; ++u) {
-                        const int r = u * kRowsAt + r0;
-                        s[u] = *reinterpret_cast<const float4*>(fbuf + r * kLpChunk + (((c >> 2) ^ ((r >> 1) & (kPer - 1))) << 2));
-                    }
-#pragma unroll
-                    for (int u = 0; u < kPer; ++u)
-                        if (u * kRowsAt + r0 < rows && col < p.l.N) ep.finish(row0 + u * kRowsAt + r0, col, s[u], extra[u]);
+                    if (full_bias && col + 32 <= p.l.N) bias_act<true>(f, v, p.l, col);
+                    else bias_act<false>(f, v, p.l, col);
+                    store_rows<O>(p.l, buf, lane, f, row0, rows, col);
                 }
             }
             ptx::tc_fence_before();

@@ -102,12 +102,17 @@ __global__ void __launch_bounds__(32 * kSmMaxWarps, 1) linear_small_kernel(Linea
     }
     s_red[warp][lane] = make_float4(acc[0], acc[1], acc[2], acc[3]);
     grid_dep_launch();
-    const LinearEpilogue<O> ep(p);
-    // thread t < 4 T of the first CTA ends up with token t / 4, features 4 (t % 4) ...: what it needs besides the sums
-    const int tok = tid >> 2, col = n0 + (tid & 3) * 4;
-    const bool ends = part == 0 && tid < 32 && tok < T && col < p.N;
-    typename LinearEpilogue<O>::Extra extra;
-    if (ends) extra = ep.fetch(tok, col);
+    // lane l of the first warp ends up with tokens l / 16 + 2 u, feature l % 16: what that needs besides the sums
+    const int col = n0 + (lane & 15), tok0 = lane >> 4;
+    const bool ends = part == 0 && warp == 0 && col < p.N;
+    __nv_bfloat16 bias = __float2bfloat16_rn(0.f);
+    O residual[4];
+    if (ends) {
+        if (p.bias != nullptr) bias = reinterpret_cast<const __nv_bfloat16*>(p.bias)[col];
+        if (p.residual != nullptr)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) residual[u] = reinterpret_cast<const O*>(p.residual)[(int64_t)min(tok0 + 2 * u, T - 1) * p.ldr + col];
+    }
     __syncthreads();
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
     if (warp == 0) {
@@ -141,7 +146,16 @@ __global__ void __launch_bounds__(32 * kSmMaxWarps, 1) linear_small_kernel(Linea
         s_out[t][lr + 8] = sum.z;
         s_out[t + 1][lr + 8] = sum.w;
         __syncwarp();
-        if (ends) ep.finish(tok, col, *reinterpret_cast<const float4*>(&s_out[tok][(tid & 3) * 4]), extra);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int k = tok0 + 2 * u;
+            if (!ends || k >= T) continue;
+            float v = s_out[k][lane & 15];
+            if (p.bias != nullptr) v += linear_f32(bias);
+            v = linear_act(v, p.act);
+            if (p.residual != nullptr) v += linear_f32(residual[u]);
+            linear_store(reinterpret_cast<O*>(p.y) + k * p.ldy + col, v);
+        }
     }
 }
 

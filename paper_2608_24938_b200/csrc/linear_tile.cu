@@ -22,12 +22,14 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kLtThreads = 192;  // warp 0: TMA producer, warp 1: MMA issuer, warps 2-5: accumulator rows; all: epilogue
+constexpr int kLtEpiWarps = 8;  // two per quadrant of the accumulator's lanes
+constexpr int kLtThreads = 64 + 32 * kLtEpiWarps;  // warp 0: TMA producer, warp 1: MMA issuer, the others: epilogue
 constexpr int kLtMaxStages = 12;
 constexpr int kLtBK = kGemmBK;
 
-template <typename O>
-__global__ void __launch_bounds__(kLtThreads) linear_tile_kernel(const __grid_constant__ LinearTileParams p) {
+// WHOLE: every group of four outputs is whole and aligned
+template <typename O, int SPLIT, bool WHOLE>
+__global__ void __launch_bounds__(kLtThreads, 2) linear_tile_kernel(const __grid_constant__ LinearTileParams p) {
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t full_bar[kLtMaxStages];
     __shared__ __align__(8) uint64_t empty_bar[kLtMaxStages];
@@ -38,7 +40,8 @@ __global__ void __launch_bounds__(kLtThreads) linear_tile_kernel(const __grid_co
         reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const int warp = ptx::warp_index(), lane = threadIdx.x & 31;
     cg::cluster_group cluster = cg::this_cluster();
-    const int split = p.plan.split, bn = p.plan.bn, stages = p.plan.stages, rank = (int)cluster.block_rank();
+    constexpr int split = SPLIT;
+    const int bn = p.plan.bn, stages = p.plan.stages, rank = (int)cluster.block_rank();
     const int nt = (p.l.N + bn - 1) / bn, tile = (int)blockIdx.x / split;
     const int n0 = tile % nt * bn;
     const int64_t row0 = (int64_t)(tile / nt) * kTileM;
@@ -71,6 +74,8 @@ __global__ void __launch_bounds__(kLtThreads) linear_tile_kernel(const __grid_co
     const int a_bytes = p.plan.a_rows * kLtBK * 2, stage_bytes = a_bytes + bn * kLtBK * 2;
     const int rows = (int)min((int64_t)kTileM, p.l.T - row0);
     const int part_ld = bn + 4;  // floats: 16-byte aligned rows, the rows of a quarter warp in distinct banks
+    const LinearEpilogue<O> ep(p.l);
+    LinearReduce<SPLIT, O, 32 * kLtEpiWarps, WHOLE> reduce(ep, rows, bn, row0, n0, rank, (int)threadIdx.x - 64);
 
     if (warp == 0) {
         if (ptx::elect_one()) {
@@ -111,15 +116,16 @@ __global__ void __launch_bounds__(kLtThreads) linear_tile_kernel(const __grid_co
         }
         __syncwarp();
     } else {
+        reduce.begin();  // bias and residual: on their way while the tile is multiplied
         // partial tile -> shared memory (the ring is free once every MMA has completed)
-        const int q = warp & 3;
+        const int q = warp & 3, half = (warp - 2) >> 2;
         int ok = 1;
         if (lane == 0) ok = ptx::mbar_wait_local(&done_bar, 0, abort_flag, p.l.status, 4) ? 1 : 0;
         ok = __shfl_sync(0xffffffffu, ok, 0);
         if (ok && q * 32 < rows) {
             ptx::tc_fence_after();
             float* dst = reinterpret_cast<float*>(tiles) + (size_t)(q * 32 + lane) * part_ld;
-            for (int c = 0; c < bn; c += 32) {
+            for (int c = 32 * half; c < bn; c += 64) {
                 uint32_t v[32];
                 ptx::tmem_ld32(tmem_base + c + ((uint32_t)(q * 32) << 16), v);
                 ptx::tmem_ld_wait();
@@ -135,24 +141,7 @@ __global__ void __launch_bounds__(kLtThreads) linear_tile_kernel(const __grid_co
     __syncthreads();
     if (abort_s) __nanosleep(100000);  // let any copy still in flight land before shared memory is released
     cluster.sync();                    // every part of the tile is in place
-    {
-        const LinearEpilogue<O> ep(p.l);
-        const int cols = bn / 4;
-        for (int i = rank * kLtThreads + threadIdx.x; i < rows * cols; i += split * kLtThreads) {
-            const int r = i / cols, c = i % cols * 4;
-            if (n0 + c >= p.l.N) continue;
-            const typename LinearEpilogue<O>::Extra extra = ep.fetch(row0 + r, n0 + c);
-            float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int k = 0; k < split; ++k) {
-                const float4 v = *reinterpret_cast<const float4*>(cluster.map_shared_rank(reinterpret_cast<float*>(tiles), k) + (size_t)r * part_ld + c);
-                s.x += v.x;
-                s.y += v.y;
-                s.z += v.z;
-                s.w += v.w;
-            }
-            ep.finish(row0 + r, n0 + c, s, extra);
-        }
-    }
+    if (warp >= 2) reduce.run(reinterpret_cast<const float*>(tiles), part_ld, 0, 1);
     grid_dep_launch();
     cluster.sync();  // no CTA leaves while its part may still be read
     if (warp == 1) {
@@ -163,19 +152,26 @@ __global__ void __launch_bounds__(kLtThreads) linear_tile_kernel(const __grid_co
 
 }  // namespace
 
+// 64 features per tile, and K split while two CTAs per SM have room for the parts and a part has four k-blocks. Where 64 features leave
+// no room to split, 128 and a split in two take less operand traffic. On the GPU, with bias and residual, 64 features / 128 in two:
+// 64 x 14336 x 4096 (tokens x features x K) 25.9 / 24.6 us, 128 x 14336 x 4096 31.7 / 28.4, 512 x 4096 x 4096 26.9 / 23.3; the other way
+// 64 x 4096 x 4096 in 64 x 4 parts / 128 x 2 11.0 / 13.1, 256 x 4096 x 4096 16.9 / 20.1, 1024 x 2048 x 768 10.8 / 12.1.
 LinearTilePlan linear_tile_plan(int64_t T, int N, int K, int sms) {
     LinearTilePlan q{};
     q.a_rows = (int)std::min<int64_t>(kTileM, (T + 15) / 16 * 16);
     const int nkb = (K + kLtBK - 1) / kLtBK;
-    const int64_t mt = (T + kTileM - 1) / kTileM;
-    q.bn = N <= 32 ? 32 : N <= 64 ? 64 : 128;
-    const int64_t tiles = mt * ((N + q.bn - 1) / q.bn);
+    q.bn = N <= 32 ? 32 : 64;
+    int64_t tiles = (T + kTileM - 1) / kTileM * ((N + q.bn - 1) / q.bn);
     q.split = 1;
-    while (q.split < 8 && tiles * q.split * 2 <= 2 * sms && nkb >= 8 * q.split) q.split *= 2;
+    const int64_t wide = (T + kTileM - 1) / kTileM * ((N + 127) / 128);
+    if (tiles > sms && wide <= sms && nkb >= 16) {
+        q.bn = 128;
+        tiles = wide;
+    }
+    while (q.split < 8 && tiles * q.split <= sms && nkb >= 8 * q.split) q.split *= 2;
     const int stage_bytes = (q.a_rows + q.bn) * kLtBK * 2;
     const int per = (nkb + q.split - 1) / q.split;
-    const int room = 104 * 1024;  // two CTAs per SM
-    q.stages = std::max(2, std::min(std::min(kLtMaxStages, per), room / stage_bytes));
+    q.stages = std::max(2, std::min(std::min(kLtMaxStages, per), 104 * 1024 / stage_bytes));
     // the ring, with what the last stage's 128 operand rows reach behind it; then the partial tile
     const size_t ring = (size_t)q.stages * stage_bytes + std::max(0, kTileM * kLtBK * 2 - stage_bytes);
     q.smem = std::max(ring, (size_t)q.a_rows * (q.bn + 4) * sizeof(float)) + 1024;
@@ -183,6 +179,19 @@ LinearTilePlan linear_tile_plan(int64_t T, int N, int K, int sms) {
     // for columns that a CTA of another cluster holds while that one waits for its own cluster's barrier
     q.smem = std::max(q.smem, (size_t)77 * 1024);
     return q;
+}
+
+// Whether the tiles of 256 x 256 on CTA pairs (linear_pair.cu) are the faster ones. Those take a third less operand traffic, but whole
+// rounds of items and a longer way in and out: about 0.31 us per k-block of a round and 9 us; the tiles here what they load at
+// 18 TB/s and 6 us. Measured, pairs / tiles: 512 x 4096 x 4096 27.9 / 22.9 us, 1024 x 4096 x 4096 30.1 / 49.1, 300 x 14336 x 4096
+// 48.7 / 77.6, 1024 x 2048 x 768 12.7 / 10.6, 2048 x 768 x 2048 18.0 / 16.3.
+bool linear_prefers_pairs(int64_t T, int N, int K, int sms) {
+    const int64_t nkb = (K + kLtBK - 1) / kLtBK;
+    const int64_t items = (T + 255) / 256 * ((N + 255) / 256), pairs = std::max(1, sms / 2), rounds = (items + pairs - 1) / pairs;
+    const LinearTilePlan q = linear_tile_plan(T, N, K, sms);
+    const double tiles = (double)((T + kTileM - 1) / kTileM) * (double)((N + q.bn - 1) / q.bn);
+    const double t_tile = tiles * (double)nkb * (q.a_rows + q.bn) * (kLtBK * 2) / 18e6 + 6.0;
+    return 0.31 * (double)(rounds * nkb) + 9.0 < t_tile;
 }
 
 cudaError_t launch_linear_tile(const LinearTileParams& p, bool out_bf16, cudaStream_t s) {
@@ -193,7 +202,14 @@ cudaError_t launch_linear_tile(const LinearTileParams& p, bool out_bf16, cudaStr
         const cudaError_t e = ensure_smem(kernel, q.smem);
         return e != cudaSuccess ? e : launch_pdl_cluster(kernel, (unsigned)grid, kLtThreads, q.smem, q.split, s, p);
     };
-    return out_bf16 ? go(linear_tile_kernel<__nv_bfloat16>) : go(linear_tile_kernel<float>);
+    auto pick = [&](auto one, auto two, auto four, auto eight) {
+        return q.split == 1 ? go(one) : q.split == 2 ? go(two) : q.split == 4 ? go(four) : go(eight);
+    };
+    const bool whole = out_bf16 ? LinearEpilogue<__nv_bfloat16>(p.l).whole() : LinearEpilogue<float>(p.l).whole();
+#define EXFOLD_LT(O, W) pick(linear_tile_kernel<O, 1, W>, linear_tile_kernel<O, 2, W>, linear_tile_kernel<O, 4, W>, linear_tile_kernel<O, 8, W>)
+    if (out_bf16) return whole ? EXFOLD_LT(__nv_bfloat16, true) : EXFOLD_LT(__nv_bfloat16, false);
+    return whole ? EXFOLD_LT(float, true) : EXFOLD_LT(float, false);
+#undef EXFOLD_LT
 }
 
 }  // namespace exfold
