@@ -362,11 +362,13 @@ int exfold_moe_decode_routed(const exfold_layer *layer, const void *x, const int
  * inputs; fp32 or bf16 for bf16). Sums, epilogue and activation in fp32, one rounding at the end. bias and residual may be
  * NULL. The ld fields are the distances between rows in elements (0: dense). residual may be y itself (the same rows and
  * distance); y overlaps no other operand.
- * Any sizes from 1 (in, out <= 2^24, T in [0, 2^24], T = 0 writes nothing). bf16 operands on the tensor cores need x and w
- * 16-byte aligned and ldx, ldw multiples of 8 elements; others, and fp32, run on a CUDA-core kernel.
+ * Any sizes from 1 (in, out <= 2^24, T in [0, 2^24], T = 0 writes nothing). bf16 products run on the tensor cores: with ldx
+ * and ldw multiples of 8 elements and x and w 16-byte aligned the operands are read in place; where a distance is no multiple
+ * of 8, x and w are first copied to aligned rows in the workspace; operands that only start unaligned, and fp32 ones, run on
+ * a CUDA-core kernel.
  * Results do not depend on other calls: no atomics, sums in a fixed order for the given sizes.
- * Workspace: exfold_linear_workspace_bytes (256-byte aligned; its first 256 bytes are the status record of
- * exfold_device_status). Calls that share a workspace must be ordered on one stream.
+ * Workspace: exfold_linear_workspace_bytes of the same description (256-byte aligned; its first 256 bytes are the status
+ * record of exfold_device_status). Calls that share a workspace must be ordered on one stream.
  */
 enum { EXFOLD_ACT_NONE = 0, EXFOLD_ACT_RELU = 1, EXFOLD_ACT_GELU = 2, EXFOLD_ACT_GELU_TANH = 3, EXFOLD_ACT_SILU = 4 };
 typedef struct {

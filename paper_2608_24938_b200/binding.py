@@ -484,11 +484,11 @@ _LINEAR_DTYPES = {torch.float32: EXFOLD_F32, torch.bfloat16: EXFOLD_BF16}
 
 
 def _rows(t: torch.Tensor, dtype, rows: int, cols: int) -> int:
-    """Row distance of a matrix whose rows are contiguous (0: of no account)."""
+    """Row distance of a matrix whose rows are contiguous (0: dense)."""
     assert t.dtype == dtype and t.shape == (rows, cols), f"expected {dtype} {(rows, cols)}, got {t.dtype} {tuple(t.shape)}"
     ld, step = t.stride()
     assert step == 1 or cols == 1, "rows must be contiguous"
-    if rows <= 1:
+    if rows <= 1 and not cols <= ld < 1 << 31:
         return 0
     assert ld >= cols, "rows must not overlap"
     return ld
@@ -503,10 +503,10 @@ def exfold_linear_workspace_bytes(desc: exfold_linear_desc, max_tokens: int) -> 
     return int(lib.exfold_linear_workspace_bytes(C.byref(desc), max_tokens))
 
 
-def alloc_linear_workspace(in_features: int, out_features: int, max_tokens: int, dtype, out_dtype=None,
-                           device="cuda") -> torch.Tensor:
-    """Workspace of exfold_linear for products of this shape with up to max_tokens rows and any row distances."""
-    desc = exfold_linear_desc(in_features, out_features, _LINEAR_DTYPES[dtype], _LINEAR_DTYPES[out_dtype or dtype], 0, 0, 0, 0, 0)
+def alloc_linear_workspace(in_features: int, out_features: int, max_tokens: int, dtype, out_dtype=None, device="cuda",
+                           ldx: int = 0, ldw: int = 0) -> torch.Tensor:
+    """Workspace of exfold_linear for products of this shape with up to max_tokens rows, ldx and ldw elements apart (0: dense)."""
+    desc = exfold_linear_desc(in_features, out_features, _LINEAR_DTYPES[dtype], _LINEAR_DTYPES[out_dtype or dtype], 0, ldx, ldw, 0, 0)
     n = exfold_linear_workspace_bytes(desc, max_tokens)
     if n == 0:
         raise ExfoldError(EXFOLD_ERR_INVALID_ARG, "exfold_linear_workspace_bytes")

@@ -1248,9 +1248,17 @@ static bool valid_linear(const exfold_linear_desc* d) {
     return ld(d->ldx, d->in_features) && ld(d->ldw, d->in_features) && ld(d->ldy, d->out_features) && ld(d->ldr, d->out_features);
 }
 
+// bf16 rows that no tensor map takes are copied to rows of this many elements first
+static int64_t packed_row(const exfold_linear_desc* d) { return (d->in_features + 15) / 16 * 16; }
+static bool linear_packs(const exfold_linear_desc* d) {
+    return d->dtype == EXFOLD_BF16 && (((d->ldx ? d->ldx : d->in_features) | (d->ldw ? d->ldw : d->in_features)) & 7) != 0;
+}
+
 size_t exfold_linear_workspace_bytes(const exfold_linear_desc* desc, int64_t max_tokens) {
     if (!valid_linear(desc) || max_tokens < 0 || max_tokens > (int64_t)1 << 24) return 0;
-    return sizeof(DeviceStatus);
+    if (!linear_packs(desc)) return sizeof(DeviceStatus);
+    return sizeof(DeviceStatus) + align_up((size_t)packed_row(desc) * 2 * max_tokens, 256) +
+           align_up((size_t)packed_row(desc) * 2 * desc->out_features, 256);
 }
 
 int exfold_linear(const exfold_linear_desc* desc, const void* x, const void* w, const void* bias, const void* residual,
@@ -1272,6 +1280,13 @@ int exfold_linear(const exfold_linear_desc* desc, const void* x, const void* w, 
     p.status = at<DeviceStatus>(ws, 0);
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
     PdlScope pdl_scope(true);
+    if (linear_packs(desc)) {
+        char* xp = at<char>(ws, sizeof(DeviceStatus));
+        char* wp = xp + align_up((size_t)packed_row(desc) * 2 * T, 256);
+        EXFOLD_CUDA(launch_linear_pack(p, xp, wp, (int)packed_row(desc), sm_count(), s));
+        p.x = x = xp; p.w = w = wp;
+        p.K = (int)packed_row(desc); p.ldx = p.ldw = p.K;
+    }
     if (bf16 && aligned16(x) && aligned16(w) && ((p.ldx | p.ldw) & 7) == 0) {
         if (linear_small_fits(p)) {
             EXFOLD_CUDA(launch_linear_small(p, out_bf16, sm_count(), s));

@@ -480,9 +480,11 @@ struct LinearParams {
     int64_t T;
     int K, N, act;
     int64_t ldx, ldw, ldy, ldr;
-    DeviceStatus* status;  // cleared by the call's first kernel
+    DeviceStatus* status;  // cleared by the kernel, which is the call's first (or follows one that did)
 };
 cudaError_t launch_linear_simt(const LinearParams& p, bool bf16, bool out_bf16, int sms, cudaStream_t s);
+// Copies of x and w (bf16) with rows of `to` elements, zeros behind K (linear.cu)
+cudaError_t launch_linear_pack(const LinearParams& p, void* xp, void* wp, int to, int sms, cudaStream_t s);
 // bf16, at most 8 tokens (linear_small.cu)
 bool linear_small_fits(const LinearParams& p);
 cudaError_t launch_linear_small(const LinearParams& p, bool out_bf16, int sms, cudaStream_t s);

@@ -1,5 +1,14 @@
-// Dense product with bias, activation and residual in its epilogue, y = act(x W^T + b) + r: the CUDA-core kernel, for fp32
-// operands and for bf16 ones that the tensor-core kernels cannot load.
+// Dense product with bias, activation and residual in its epilogue, y = act(x W^T + b) + r, on the CUDA cores: fp32 operands, which
+// tensor cores would round, and bf16 ones that no tensor map takes.
+//
+//   few tokens   A warp takes 8 features x 8 tokens, its lanes along K: 16 loads of 16 bytes per lane feed 256 multiply-adds, straight
+//       from global memory (the weights of a token group after the first come from L2). The warps of a CTA split K; the 64 sums of a warp
+//       are reduced over the lanes by halving exchanges (62 shuffles) and meet in shared memory, in order.
+//   tiles        64 x 64 outputs per CTA of 128 threads, 8 x 4 of them per thread; K in steps of 16 through two shared-memory stages,
+//       the next step's loads in registers meanwhile. Rows lie along K with a pitch of 20 floats: what a quarter warp reads in 16-byte
+//       pieces hits distinct banks. Bound by those reads (shared memory returns 128 bytes per cycle; 8 x 4 outputs need 48 bytes per
+//       thread for 32 multiply-adds) and by latency: K is split over a cluster (LinearReduce) until four CTAs share an SM. 128 x 64
+//       tiles with 8 x 8 outputs per thread need 254 registers and were slower at every size: 512 x 2048 x 1024 75 us against 69.
 #include <algorithm>
 
 #include "common.cuh"
@@ -9,141 +18,262 @@ namespace exfold {
 
 namespace {
 
-constexpr int kLsThreads = 256;
-constexpr int kLsBK = 16;
-
-// Two products at once: the packed form issues half as many instructions
-__device__ __forceinline__ void fma2(float2& c, const float2& a, const float2& b) {
-    asm("fma.rn.f32x2 %0, %1, %2, %0;"
-        : "+l"(reinterpret_cast<unsigned long long&>(c))
-        : "l"(reinterpret_cast<const unsigned long long&>(a)), "l"(reinterpret_cast<const unsigned long long&>(b)));
+// Four elements at p, of which the first `left` exist; the rest are zeros. VEC: aligned to four
+template <bool VEC, typename T>
+__device__ __forceinline__ float4 load4(const T* p, int left) {
+    if (VEC && left >= 4) return linear_load4(p);
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (left > 0) v.x = linear_f32(p[0]);
+    if (left > 1) v.y = linear_f32(p[1]);
+    if (left > 2) v.z = linear_f32(p[2]);
+    if (left > 3) v.w = linear_f32(p[3]);
+    return v;
 }
 
-// BM x BN outputs per block, K in steps of 16 through shared memory (transposed, double buffered); a thread owns TM x TN of
-// them. VEC: rows of x and w can be read four elements at a time.
-template <typename T, typename O, int BM, int BN, bool VEC>
+// ---------------------------------------------------------------- few tokens
+constexpr int kLfWarps = 8, kLfTile = 8;  // features, and tokens, of a CTA
+
+// Sum over the lanes of each of 64 values; lane l ends up with those of values l and l + 32 in v[0] and v[32]
+__device__ __forceinline__ void halve64(float (&v)[64], int lane) {
+#pragma unroll
+    for (int half = 0; half < 64; half += 32)
+#pragma unroll
+        for (int n = 16; n > 0; n >>= 1) {
+            const bool up = (lane & n) != 0;
+#pragma unroll
+            for (int j = 0; j < n; ++j) {
+                const float give = up ? v[half + j] : v[half + j + n], keep = up ? v[half + j + n] : v[half + j];
+                v[half + j] = keep + __shfl_xor_sync(0xffffffffu, give, n);
+            }
+        }
+}
+
+template <typename T, typename O, bool VEC>
+__global__ void __launch_bounds__(32 * kLfWarps) linear_few_kernel(LinearParams p) {
+    __shared__ float s_sum[kLfWarps][64];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = (int)blockDim.x >> 5;
+    const int fblocks = (p.N + kLfTile - 1) / kLfTile;
+    const int n0 = (int)(blockIdx.x % fblocks) * kLfTile;
+    const int64_t m0 = (int64_t)(blockIdx.x / fblocks) * kLfTile;
+    const T* x = reinterpret_cast<const T*>(p.x) + lane * 4;
+    const T* w = reinterpret_cast<const T*>(p.w) + lane * 4;
+    grid_dep_launch();
+    grid_dep_wait();
+    if (blockIdx.x == 0 && threadIdx.x < 4) reinterpret_cast<int*>(p.status)[threadIdx.x] = 0;
+    // thread t < 64 ends up with token t / 8, feature t % 8
+    const int col = n0 + (int)(threadIdx.x & 7);
+    const int64_t tok = m0 + (threadIdx.x >> 3);
+    const bool ends = threadIdx.x < 64 && col < p.N && tok < p.T;
+    T bias{};
+    O residual{};
+    float acc[64];  // [feature][token]: value 8 f + t
+#pragma unroll
+    for (int i = 0; i < 64; ++i) acc[i] = 0.f;
+    for (int k0 = warp * 128; k0 < p.K; k0 += warps * 128) {
+        const int left = p.K - k0 - lane * 4;
+        float4 a[8], b[8];
+#pragma unroll
+        for (int f = 0; f < 8; ++f) a[f] = load4<VEC>(w + min(n0 + f, p.N - 1) * p.ldw + k0, left);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) b[t] = load4<VEC>(x + min(m0 + t, p.T - 1) * p.ldx + k0, left);
+#pragma unroll
+        for (int f = 0; f < 8; ++f)
+#pragma unroll
+            for (int t = 0; t < 8; ++t)
+                acc[8 * f + t] += fmaf(a[f].w, b[t].w, fmaf(a[f].z, b[t].z, fmaf(a[f].y, b[t].y, a[f].x * b[t].x)));
+    }
+    if (ends) {
+        if (p.bias != nullptr) bias = reinterpret_cast<const T*>(p.bias)[col];
+        if (p.residual != nullptr) residual = reinterpret_cast<const O*>(p.residual)[tok * p.ldr + col];
+    }
+    halve64(acc, lane);
+    s_sum[warp][lane] = acc[0];
+    s_sum[warp][lane + 32] = acc[32];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 64; i += blockDim.x) {  // one pass with two warps or more
+        const int n = n0 + (i & 7);
+        const int64_t m = m0 + (i >> 3);
+        if (n >= p.N || m >= p.T) continue;
+        const int at = (i & 7) * 8 + (i >> 3);
+        float v = s_sum[0][at];
+        for (int q = 1; q < warps; ++q) v += s_sum[q][at];
+        if (i != (int)threadIdx.x) {
+            if (p.bias != nullptr) bias = reinterpret_cast<const T*>(p.bias)[n];
+            if (p.residual != nullptr) residual = reinterpret_cast<const O*>(p.residual)[m * p.ldr + n];
+        }
+        if (p.bias != nullptr) v += linear_f32(bias);
+        v = linear_act(v, p.act);
+        if (p.residual != nullptr) v += linear_f32(residual);
+        linear_store(reinterpret_cast<O*>(p.y) + m * p.ldy + n, v);
+    }
+}
+
+// ---------------------------------------------------------------- tiles
+constexpr int kLsThreads = 128;
+constexpr int kLsBM = 64, kLsBN = 64, kLsBK = 16, kLsPitch = kLsBK + 4;
+
+template <typename T, typename O, bool VEC, int SPLIT>
 __global__ void __launch_bounds__(kLsThreads) linear_simt_kernel(LinearParams p) {
-    constexpr int TM = BM / 16, TN = BN / 16;
-    constexpr int kA = BM * kLsBK / 4 / kLsThreads, kB = BN * kLsBK / 4 / kLsThreads;  // groups of four elements per thread
-    __shared__ __align__(16) float sa[2][kLsBK][BM + 4];
-    __shared__ __align__(16) float sb[2][kLsBK][BN + 4];
+    constexpr int BM = kLsBM, TX = 16, TY = kLsThreads / TX, TM = BM / TY, TN = kLsBN / TX;
+    constexpr int kLoadsA = BM * kLsBK / 4 / kLsThreads, kLoadsB = kLsBN * kLsBK / 4 / kLsThreads;  // of four elements
+    constexpr int kStage = (BM + kLsBN) * kLsPitch, kPart = kLsBN + 1;
+    // two stages of both operands; then the partial tile
+    __shared__ __align__(16) float smem[2 * kStage > BM * kPart ? 2 * kStage : BM * kPart];
     const T* x = reinterpret_cast<const T*>(p.x);
     const T* w = reinterpret_cast<const T*>(p.w);
-    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
-    const int n_tiles = (p.N + BN - 1) / BN;
-    const int64_t m0 = (int64_t)(blockIdx.x / n_tiles) * BM;
-    const int n0 = (int)(blockIdx.x % n_tiles) * BN;
+    const int tid = threadIdx.x, tx = tid % TX, ty = tid / TX;
+    const int n_tiles = (p.N + kLsBN - 1) / kLsBN;
+    const int rank = (int)blockIdx.x % SPLIT, tile = (int)blockIdx.x / SPLIT;
+    const int64_t m0 = (int64_t)(tile / n_tiles) * BM;
+    const int n0 = tile % n_tiles * kLsBN;
+    const int steps = (p.K + kLsBK - 1) / kLsBK, s0 = (int)((int64_t)rank * steps / SPLIT), s1 = (int)((int64_t)(rank + 1) * steps / SPLIT);
     grid_dep_launch();
     grid_dep_wait();
     if (blockIdx.x == 0 && tid < 4) reinterpret_cast<int*>(p.status)[tid] = 0;
-    float ra[kA][4], rb[kB][4];
-    auto fetch = [&](const T* base, int64_t row, int64_t rows, int64_t ld, int k, float (&v)[4]) {
+    const LinearEpilogue<O> ep(p);
+    LinearReduce<SPLIT, O, kLsThreads, false, T> reduce(ep, (int)min((int64_t)BM, p.T - m0), kLsBN, m0, n0, rank, tid);
+    // thread t loads rows t / 4 + 32 u, four elements at 4 (t % 4)
+    const int lrow = tid >> 2, lk = (tid & 3) * 4;
+    const T* px[kLoadsA];
+    const T* pw[kLoadsB];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = 0.f;
-        if (row >= rows) return;
-        const T* src = base + row * ld + k;
-        if (VEC && k + 4 <= p.K) {
-            const float4 t = linear_load4(src);
-            v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
-        } else {
+    for (int u = 0; u < kLoadsA; ++u) px[u] = x + min(m0 + lrow + 32 * u, p.T - 1) * p.ldx + lk;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (k + j < p.K) v[j] = linear_f32(src[j]);
-        }
-    };
-    auto load = [&](int k0) {
+    for (int u = 0; u < kLoadsB; ++u) pw[u] = w + (int64_t)min(n0 + lrow + 32 * u, p.N - 1) * p.ldw + lk;
+    float4 ra[kLoadsA], rb[kLoadsB];
+    auto load = [&](int s) {
+        const int left = p.K - s * kLsBK - lk;
 #pragma unroll
-        for (int u = 0; u < kA; ++u) {
-            const int i = tid + u * kLsThreads;
-            fetch(x, m0 + i / 4, p.T, p.ldx, k0 + i % 4 * 4, ra[u]);
-        }
+        for (int u = 0; u < kLoadsA; ++u) ra[u] = load4<VEC>(px[u] + (int64_t)s * kLsBK, left);
 #pragma unroll
-        for (int u = 0; u < kB; ++u) {
-            const int i = tid + u * kLsThreads;
-            fetch(w, n0 + i / 4, p.N, p.ldw, k0 + i % 4 * 4, rb[u]);
-        }
+        for (int u = 0; u < kLoadsB; ++u) rb[u] = load4<VEC>(pw[u] + (int64_t)s * kLsBK, left);
     };
     auto store = [&](int buf) {
+        float* dst = smem + buf * kStage + lrow * kLsPitch + lk;
 #pragma unroll
-        for (int u = 0; u < kA; ++u) {
-            const int i = tid + u * kLsThreads;
+        for (int u = 0; u < kLoadsA; ++u) *reinterpret_cast<float4*>(dst + 32 * u * kLsPitch) = ra[u];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) sa[buf][i % 4 * 4 + j][i / 4] = ra[u][j];
-        }
-#pragma unroll
-        for (int u = 0; u < kB; ++u) {
-            const int i = tid + u * kLsThreads;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) sb[buf][i % 4 * 4 + j][i / 4] = rb[u][j];
-        }
+        for (int u = 0; u < kLoadsB; ++u) *reinterpret_cast<float4*>(dst + (BM + 32 * u) * kLsPitch) = rb[u];
     };
-    float2 acc[TM][TN / 2];
+    // outputs of this thread: rows ty + TY i, columns tx + TX j
+    float acc[TM][TN];
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < TN / 2; ++j) acc[i][j] = make_float2(0.f, 0.f);
-    load(0);
+        for (int j = 0; j < TN; ++j) acc[i][j] = 0.f;
+    load(s0);
     store(0);
     __syncthreads();
     int buf = 0;
-    for (int k0 = 0; k0 < p.K; k0 += kLsBK) {
-        const bool more = k0 + kLsBK < p.K;
-        if (more) load(k0 + kLsBK);
+    for (int s = s0; s < s1; ++s, buf ^= 1) {
+        if (s + 1 < s1) load(s + 1);
+        const float* sa = smem + buf * kStage + ty * kLsPitch;
+        const float* sb = smem + buf * kStage + (BM + tx) * kLsPitch;
 #pragma unroll
-        for (int k = 0; k < kLsBK; ++k) {
-            // a thread's rows and columns lie four apart from its neighbours': 16-byte reads without bank conflicts
-            float a[TM];
-            float2 b[TN / 2];
+        for (int k = 0; k < kLsBK; k += 4) {
+            float4 b[TN];
 #pragma unroll
-            for (int u = 0; u < TM / 4; ++u) {
-                const float4 v = *reinterpret_cast<const float4*>(&sa[buf][k][u * 64 + ty * 4]);
-                a[4 * u] = v.x; a[4 * u + 1] = v.y; a[4 * u + 2] = v.z; a[4 * u + 3] = v.w;
+            for (int j = 0; j < TN; ++j) b[j] = *reinterpret_cast<const float4*>(sb + TX * j * kLsPitch + k);
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                const float4 a = *reinterpret_cast<const float4*>(sa + TY * i * kLsPitch + k);
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] = fmaf(a.x, b[j].x, acc[i][j]);
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] = fmaf(a.y, b[j].y, acc[i][j]);
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] = fmaf(a.z, b[j].z, acc[i][j]);
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] = fmaf(a.w, b[j].w, acc[i][j]);
             }
-#pragma unroll
-            for (int u = 0; u < TN / 4; ++u) {
-                const float4 v = *reinterpret_cast<const float4*>(&sb[buf][k][u * 64 + tx * 4]);
-                b[2 * u] = make_float2(v.x, v.y);
-                b[2 * u + 1] = make_float2(v.z, v.w);
-            }
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int j = 0; j < TN / 2; ++j) fma2(acc[i][j], make_float2(a[i], a[i]), b[j]);
         }
-        if (more) store(buf ^ 1);
+        if (s + 1 < s1) store(buf ^ 1);
         __syncthreads();
-        buf ^= 1;
     }
-    const T* bias = reinterpret_cast<const T*>(p.bias);
-    O* y = reinterpret_cast<O*>(p.y);
-    const O* r = reinterpret_cast<const O*>(p.residual);
+    reduce.begin();
+    float* part = smem;
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-        const int n = n0 + (j >> 2) * 64 + tx * 4 + (j & 3);
-        if (n >= p.N) continue;
-        const float bv = bias != nullptr ? linear_f32(bias[n]) : 0.f;
+    for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            const int64_t m = m0 + (i >> 2) * 64 + ty * 4 + (i & 3);
-            if (m >= p.T) continue;
-            float v = linear_act(((j & 1) ? acc[i][j / 2].y : acc[i][j / 2].x) + bv, p.act);
-            if (r != nullptr) v += linear_f32(r[m * p.ldr + n]);
-            linear_store(y + m * p.ldy + n, v);
-        }
-    }
+        for (int j = 0; j < TN; ++j) part[(ty + TY * i) * kPart + tx + TX * j] = acc[i][j];
+    if (SPLIT > 1) cooperative_groups::this_cluster().sync();
+    else __syncthreads();
+    reduce.run(part, kPart, 0, 1);
+    if (SPLIT > 1) cooperative_groups::this_cluster().sync();  // no CTA leaves while its part may still be read
 }
 
 template <typename T, typename O, bool VEC>
 cudaError_t launch_simt_t(const LinearParams& p, int sms, cudaStream_t s) {
-    auto blocks = [&](int b) { return ((p.T + b - 1) / b) * ((p.N + b - 1) / b); };
-    const bool large = blocks(128) >= sms;
-    const int64_t grid = blocks(large ? 128 : 64);
-    if (grid > 0x7fffffff) return cudaErrorInvalidValue;
-    if (large) return launch_pdl(linear_simt_kernel<T, O, 128, 128, VEC>, (unsigned)grid, kLsThreads, 0, s, p);
-    return launch_pdl(linear_simt_kernel<T, O, 64, 64, VEC>, (unsigned)grid, kLsThreads, 0, s, p);
+    // few tokens / tiles: 32 x 1024 x 1024 11.1 / 15.2 us, 32 x 2000 x 2000 31.4 / 32.1, 48 x 512 x 512 5.2 / 6.2, 64 x 256 x 128 3.0 / 4.1,
+    // 64 x 1024 x 1024 19.3 / 16.0
+    if (p.T <= 32 || (p.T <= 64 && p.K <= 512)) {
+        const int64_t grid = (int64_t)((p.N + kLfTile - 1) / kLfTile) * ((p.T + kLfTile - 1) / kLfTile);
+        return launch_pdl(linear_few_kernel<T, O, VEC>, (unsigned)grid, 32 * std::max(1, std::min(kLfWarps, (p.K + 127) / 128)), 0, s, p);
+    }
+    const int64_t tiles = ((p.T + kLsBM - 1) / kLsBM) * ((p.N + kLsBN - 1) / kLsBN);
+    if (tiles > 0x0fffffff) return cudaErrorInvalidValue;
+    // 64 x 1024 x 1024 (tokens x features x K) in 1 / 2 / 4 / 8 parts 63.0 / 29.5 / 17.3 / 16.0 us, 300 x 700 x 1000 62.9 / 46.4 / 35.1 /
+    // 21.6, 1000 x 500 x 500 57.7 / 37.0 / 22.2 / 27.1, 1024 x 1000 x 2048 259 / 131 / 133 / 130
+    int split = 1;
+    while (split < 8 && tiles * split * 2 <= 4 * sms && p.K >= 4 * kLsBK * split) split *= 2;
+    auto go = [&](auto kernel) { return launch_pdl_cluster(kernel, (unsigned)(tiles * split), kLsThreads, 0, split, s, p); };
+    switch (split) {
+        case 1: return go(linear_simt_kernel<T, O, VEC, 1>);
+        case 2: return go(linear_simt_kernel<T, O, VEC, 2>);
+        case 4: return go(linear_simt_kernel<T, O, VEC, 4>);
+        default: return go(linear_simt_kernel<T, O, VEC, 8>);
+    }
+}
+
+// Rows of any alignment -> rows of `to` elements (a multiple of 8), zeros behind the K there are. Aligned 16-byte loads inside the
+// matrix, shifted to the row's start; the matrix' ends element by element.
+struct PackRows {
+    const __nv_bfloat16* src;
+    __nv_bfloat16* dst;
+    int64_t rows, ld;
+};
+__global__ void __launch_bounds__(256) pack_rows_kernel(PackRows x, PackRows w, int K, int to, DeviceStatus* status) {
+    grid_dep_launch();
+    grid_dep_wait();
+    if (blockIdx.x == 0 && threadIdx.x < 4) reinterpret_cast<int*>(status)[threadIdx.x] = 0;
+    const int chunks = to / 8;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (x.rows + w.rows) * chunks; i += (int64_t)gridDim.x * 256) {
+        int64_t r = i / chunks;
+        const int k = (int)(i - r * chunks) * 8;
+        const bool first = r < x.rows;
+        const PackRows& m = first ? x : w;
+        if (!first) r -= x.rows;
+        const __nv_bfloat16* src = m.src + r * m.ld + k;
+        const uintptr_t at = reinterpret_cast<uintptr_t>(src), low = at & ~(uintptr_t)15;
+        const uintptr_t begin = reinterpret_cast<uintptr_t>(m.src), end = reinterpret_cast<uintptr_t>(m.src + (m.rows - 1) * m.ld + K);
+        uint32_t o[4] = {0u, 0u, 0u, 0u};
+        if (k + 8 <= K && low >= begin && low + 32 <= end) {
+            const uint4 a = __ldg(reinterpret_cast<const uint4*>(low)), b = __ldg(reinterpret_cast<const uint4*>(low + 16));
+            const uint32_t v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+            const int words = (int)(at - low) >> 2, bits = ((int)(at - low) & 2) * 8;
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+                if (words == s)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[j] = __funnelshift_r(v[s + j], v[min(s + j + 1, 7)], bits);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (k + j < K) reinterpret_cast<__nv_bfloat16*>(o)[j] = src[j];
+        }
+        *reinterpret_cast<uint4*>(m.dst + r * to + k) = make_uint4(o[0], o[1], o[2], o[3]);
+    }
 }
 
 }  // namespace
+
+cudaError_t launch_linear_pack(const LinearParams& p, void* xp, void* wp, int to, int sms, cudaStream_t s) {
+    const PackRows x{reinterpret_cast<const __nv_bfloat16*>(p.x), reinterpret_cast<__nv_bfloat16*>(xp), p.T, p.ldx};
+    const PackRows w{reinterpret_cast<const __nv_bfloat16*>(p.w), reinterpret_cast<__nv_bfloat16*>(wp), p.N, p.ldw};
+    const int64_t chunks = (p.T + p.N) * (to / 8);
+    const unsigned grid = (unsigned)std::max<int64_t>(1, std::min<int64_t>((chunks + 255) / 256, (int64_t)16 * sms));
+    return launch_pdl(pack_rows_kernel, grid, 256, 0, s, x, w, p.K, to, p.status);
+}
 
 cudaError_t launch_linear_simt(const LinearParams& p, bool bf16, bool out_bf16, int sms, cudaStream_t s) {
     const uintptr_t bytes = bf16 ? 8 : 16;

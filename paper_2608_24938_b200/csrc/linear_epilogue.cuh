@@ -87,7 +87,8 @@ struct LinearEpilogue {
 // asked for ahead, the first ones by begin(), while the products are still running; all loads of U groups are in flight together
 // (those of places past the tile's end go to its last place). In a chain they made this part of a 128 x 256 tile 20 us.
 // WHOLE: every group of four outputs is whole and aligned; else a thread takes single outputs, neighbours in neighbouring lanes.
-template <int S, typename O, int THREADS, bool WHOLE>
+// B: the bias' type (groups of four: bf16).
+template <int S, typename O, int THREADS, bool WHOLE, typename B = __nv_bfloat16>
 struct LinearReduce {
     static constexpr int U = S >= 8 ? 1 : S == 1 ? 4 : 2, kStride = S * THREADS;
     const LinearEpilogue<O>& ep;
@@ -141,13 +142,13 @@ struct LinearReduce {
         }
     }
 };
-template <int S, typename O, int THREADS>
-struct LinearReduce<S, O, THREADS, false> {
+template <int S, typename O, int THREADS, typename B>
+struct LinearReduce<S, O, THREADS, false, B> {
     static constexpr int U = S >= 8 ? 2 : S == 4 ? 4 : 8, kStride = S * THREADS;
     const LinearParams& l;
     int shift, total, n0, i0;
     int64_t row0;
-    __nv_bfloat16 bias[U];
+    B bias[U];
     O residual[U];
 
     __device__ __forceinline__ LinearReduce(const LinearEpilogue<O>& e, int rows, int cols, int64_t row0_, int n0_, int me, int tid)
@@ -157,7 +158,7 @@ struct LinearReduce<S, O, THREADS, false> {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int i = min(i0 + u * kStride, total - 1), r = i >> shift, n = min(n0 + i - (r << shift), l.N - 1);
-            if (l.bias != nullptr) bias[u] = reinterpret_cast<const __nv_bfloat16*>(l.bias)[n];
+            if (l.bias != nullptr) bias[u] = reinterpret_cast<const B*>(l.bias)[n];
             if (l.residual != nullptr) residual[u] = reinterpret_cast<const O*>(l.residual)[(row0 + r) * l.ldr + n];
         }
     }

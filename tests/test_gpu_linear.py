@@ -74,7 +74,7 @@ def check(ex, T, i, o, dtype=torch.bfloat16, out=None, bias=True, residual=True,
         y.fill_(float("nan"))
     around = torch.ones_like(ybuf, dtype=torch.bool)
     around[offset:offset + T * (ldy or o)].view(T, ldy or o)[:, :o] = False
-    ws = ex.alloc_linear_workspace(i, o, T, dtype, out)
+    ws = ex.alloc_linear_workspace(i, o, T, dtype, out, ldx=ldx or 0, ldw=ldw or 0)
     ws.fill_(0xFF)
     ex.exfold_linear(x, w, y, ws, bias=b, residual=r, activation=act)
     assert ex.exfold_device_status(ws) == 0
@@ -142,6 +142,16 @@ def test_linear_in_place_residual(ex, dtype, out, T):
                                    (16, 14336, 4096), (777, 2040, 1411)])
 def test_linear_large(ex, T, i, o):
     check(ex, T, i, o, act="gelu_tanh")
+
+
+@pytest.mark.parametrize("T", [1, 9, 140, 700])
+@pytest.mark.parametrize("i", [1, 7, 9, 63, 65, 514, 1411])
+def test_linear_copied_rows(ex, T, i):
+    """bf16 rows at odd distances, from every alignment of the matrix' start; NaN before, between and behind them."""
+    for offset in range(0, 9):
+        check(ex, T, i, 136, offset=offset, ldx=i + (i + 1) % 2, ldw=i + 2 + (i + 1) % 2)
+    check(ex, T, i, 136, ldx=(i + 7) // 8 * 8, ldw=i + 3)
+    check(ex, T, i, 136, ldx=i + 3, ldw=(i + 7) // 8 * 8)
 
 
 def test_linear_zero_tokens_writes_nothing(ex):
