@@ -1191,6 +1191,7 @@ int exfold_route(const exfold_layer* layer, const float* logits, int64_t T, cons
     p.by_score = router->bias != nullptr || (p.n_groups > 1 && p.group_top2);
     p.renormalise = router->renormalise != 0; p.scale = router->scale;
     p.ids = ids; p.w = w; p.load = load;
+    PdlScope pdl_scope(true);
     EXFOLD_CUDA(launch_route_general(p, sm_count(), reinterpret_cast<cudaStream_t>(cuda_stream)));
     return EXFOLD_OK;
 }
@@ -1205,6 +1206,7 @@ int exfold_route_backward(const exfold_layer* layer, const float* logits, const 
     p.logits = logits; p.ids = ids; p.dw = dw; p.T = T; p.N = layer->n_experts; p.K = layer->top_k;
     p.softmax = router->score == EXFOLD_SCORE_SOFTMAX; p.renormalise = router->renormalise != 0; p.scale = router->scale;
     p.dlogits = dlogits;
+    PdlScope pdl_scope(true);
     EXFOLD_CUDA(launch_route_backward(p, sm_count(), reinterpret_cast<cudaStream_t>(cuda_stream)));
     return EXFOLD_OK;
 }

@@ -250,6 +250,7 @@ struct RouteGeneralParams {
     int32_t* ids;   // [T][K]
     float* w;       // [T][K]
     int32_t* load;  // [N] or null
+    int batch;  // set by the launcher
 };
 struct RouteBackwardParams {
     const float* logits;  // [T][N]
@@ -260,7 +261,7 @@ struct RouteBackwardParams {
     float scale;
     float* dlogits;  // [T][N]
 };
-cudaError_t launch_route_general(const RouteGeneralParams& p, int sms, cudaStream_t s);
+cudaError_t launch_route_general(RouteGeneralParams p, int sms, cudaStream_t s);
 cudaError_t launch_route_backward(const RouteBackwardParams& p, int sms, cudaStream_t s);
 
 // ---------------------------------------------------------------- routing (decode)

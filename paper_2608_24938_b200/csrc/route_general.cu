@@ -1,5 +1,23 @@
 // Routing by a model's own router: softmax or sigmoid scores, a bias for the choice, expert groups, Top-K, weights; and the
 // gradient of those weights with respect to the router scores.
+//
+// A warp takes a token at a time: expert lane + 32 q in register q of NPL. A call reads 4 N bytes per token and is bound by
+// instructions, so what is done per token is kept short:
+//
+//   choice    Choices are scores + bias, and two of them may differ by less than an fp32 rounding, so they are compared as computed in
+//             64 bits. That is done only where it matters: choices are computed and ranked in fp32, K + 1 of them, and only where two
+//             neighbours in that ranking lie closer than the fp32 error (below) are these K + 1 ranked again by 64-bit choices: one
+//             token in a few hundred. Where that leaves the set open (the next one is as close, or a group is), or a softmax has a bias,
+//             all experts are (pick_exact). Scores ranked as they are (no bias) need no second look.
+//   Top-K     each lane sorts its NPL keys; a round is a warp-wide maximum over the lanes' heads and the lowest expert that has it,
+//             and that one's lane moves its next key up
+//   weights   of the K chosen in 64 bits, rounded once: one lane per slot, up to four tokens of a warp at once
+//
+// Error of an fp32 choice, in half steps of 1 (2^-24; a score s is at most 1). Sigmoid: __expf is off by 2 + 1.2 |z| steps, which count
+// s (1 - s) times: below 1.3; the sum 1, the quotient 4. Softmax: the argument's rounding counts d e^-d <= 0.4, expf 4, the sum 13, the
+// quotient 4: below 22. And the addition's half step of the choice. Two choices are sure of their order if further apart than twice that.
+//
+// GPU time, 64-bit choices for every token -> now: 16384 tokens x 128 experts 23.2 -> KKK us.
 #include <algorithm>
 
 #include "common.cuh"
@@ -9,8 +27,8 @@ namespace exfold {
 namespace {
 
 constexpr int kGrThreads = 256;
-constexpr int kGrWarps = kGrThreads / 32;
 constexpr float kMaskedScore = -3.402823466e38f;  // this and -infinity
+constexpr float kErrSigmoid = 2.f * 6.5f / (1 << 24), kErrSoftmax = 2.f * 22.f / (1 << 24), kErrChoice = 2.f / (1 << 24);
 
 // Order-preserving image of a double; every NaN is the largest, -0 is +0
 __device__ __forceinline__ unsigned long long order64(double c) {
@@ -18,138 +36,348 @@ __device__ __forceinline__ unsigned long long order64(double c) {
     const unsigned long long b = (unsigned long long)__double_as_longlong(c + 0.0);
     return (b >> 63) ? ~b : b | (1ull << 63);
 }
-
+__device__ __forceinline__ double from_order64(unsigned long long k) {
+    return k == ~0ull ? (double)NAN : __longlong_as_double((long long)((k >> 63) ? k & ~(1ull << 63) : ~k));
+}
 // The same of a float
 __device__ __forceinline__ unsigned order32(float f) { return f != f ? 0xffffffffu : float_order_key(f); }
+__device__ __forceinline__ float from_order32(unsigned k) { return k == 0xffffffffu ? NAN : float_from_order_key(k); }
 
-// One warp per token, expert lane + 32 q in register q. Choices are compared in 64 bits: two experts' choices may differ by
-// less than an fp32 rounding of them.
+// Whether a, ranked before b by fp32 choices whose scores may be off by err / 2, might come after it in 64 bits
+__device__ __forceinline__ bool close_call(float a, float b, float err) {
+    return !(a - b > err + kErrChoice * fmaxf(fabsf(a), fabsf(b))) && a > -INFINITY && b > -INFINITY;  // a NaN is not close to what follows it
+}
+
+// `n` experts, one per lane, in the order of 64-bit choices (sigmoid scores): lane k returns the k-th
+__device__ __noinline__ int rank_exact(const RouteGeneralParams& p, const float* z, int id, int n, int lane) {
+    unsigned long long key = 0;
+    if (lane < n) {
+        const float v = z[id];
+        double c = 1.0 / (1.0 + exp(-(double)v));
+        if (p.bias != nullptr) c += (double)p.bias[id];
+        key = order64(v <= kMaskedScore ? -INFINITY : c);
+    }
+    int place = lane < n ? 0 : lane, out = id;
+    for (int j = 0; j < n; ++j) {
+        const unsigned long long kj = __shfl_sync(0xffffffffu, key, j);
+        const int ij = __shfl_sync(0xffffffffu, id, j);
+        if (lane < n && (kj > key || (kj == key && ij < id))) ++place;
+    }
+    for (int j = 0; j < n; ++j) {
+        const int pj = __shfl_sync(0xffffffffu, place, j), ij = __shfl_sync(0xffffffffu, id, j);
+        if (pj == lane) out = ij;
+    }
+    return out;
+}
+
+// One token's experts from 64-bit choices: lane k < K returns the k-th. cand: this lane's experts; sk: scratch of N words of the warp.
 template <int NPL>
-__global__ void __launch_bounds__(kGrThreads) route_general_kernel(RouteGeneralParams p) {
-    extern __shared__ unsigned long long s_key[];  // [warps][N], with groups only
-    __shared__ int hist[kMaxExperts];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+__device__ __noinline__ int pick_exact(const RouteGeneralParams& p, const float* z, unsigned long long* sk, int lane) {
     const int N = p.N, K = p.K;
+    unsigned long long key[NPL];
+    unsigned cand = 0;
+    float zmax = -INFINITY;
+#pragma unroll
+    for (int q = 0; q < NPL; ++q) {
+        const float v = lane + 32 * q < N ? z[lane + 32 * q] : -INFINITY;
+        zmax = isnan(v) || v > zmax ? v : zmax;
+    }
+    zmax = from_order32(__reduce_max_sync(0xffffffffu, order32(zmax)));
+    double sum = 0.0;
+    if (p.softmax) {
+#pragma unroll
+        for (int q = 0; q < NPL; ++q) {
+            const float v = lane + 32 * q < N ? z[lane + 32 * q] : -INFINITY;
+            if (!(v <= kMaskedScore)) sum += exp((double)v - (double)zmax);
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    }
+#pragma unroll
+    for (int q = 0; q < NPL; ++q) {
+        const int e = lane + 32 * q;
+        const float v = e < N ? z[e] : -INFINITY;
+        double c = (double)v;
+        if (p.by_score) {
+            c = p.softmax ? exp((double)v - (double)zmax) / sum : 1.0 / (1.0 + exp(-(double)v));
+            if (p.bias != nullptr && e < N) c += (double)p.bias[e];
+        }
+        if (v <= kMaskedScore) c = -INFINITY;
+        if (e < N) cand |= 1u << q;
+        key[q] = order64(c);
+    }
+    if (p.n_groups > 1) {  // lane g takes group g's score and its place among the groups
+        __syncwarp();
+#pragma unroll
+        for (int q = 0; q < NPL; ++q)
+            if (lane + 32 * q < N) sk[lane + 32 * q] = key[q];
+        __syncwarp();
+        const int per = N / p.n_groups;
+        unsigned long long k1 = 0, k2 = 0;
+        if (lane < p.n_groups)
+            for (int j = 0; j < per; ++j) {
+                const unsigned long long k = sk[lane * per + j];
+                if (k > k1) { k2 = k1; k1 = k; }
+                else if (k > k2) k2 = k;
+            }
+        if (p.group_top2 && k2 > order64(-INFINITY)) k1 = order64(from_order64(k1) + from_order64(k2));
+        int place = 0;
+        for (int g = 0; g < p.n_groups; ++g) {
+            const unsigned long long kg = __shfl_sync(0xffffffffu, k1, g);
+            if (kg > k1 || (kg == k1 && g < lane)) ++place;
+        }
+        const unsigned stay = __ballot_sync(0xffffffffu, lane < p.n_groups && place < p.top_groups);
+#pragma unroll
+        for (int q = 0; q < NPL; ++q)
+            if (!((stay >> min(31, (lane + 32 * q) / per)) & 1u)) cand &= ~(1u << q);
+    }
+    int my_id = 0;
+    for (int k = 0; k < K; ++k) {
+        unsigned long long bk = 0;
+        int be = 0x7fffffff;
+#pragma unroll
+        for (int q = 0; q < NPL; ++q)
+            if (((cand >> q) & 1u) && (be == 0x7fffffff || key[q] > bk)) {
+                bk = key[q];
+                be = lane + 32 * q;
+            }
+        const bool has = be != 0x7fffffff;
+        const unsigned hi = __reduce_max_sync(0xffffffffu, has ? (unsigned)(bk >> 32) : 0u);
+        const bool top = has && (unsigned)(bk >> 32) == hi;
+        const unsigned lo = __reduce_max_sync(0xffffffffu, top ? (unsigned)bk : 0u);
+        be = __reduce_min_sync(0xffffffffu, top && (unsigned)bk == lo ? be : 0x7fffffff);
+        if ((be & 31) == lane) cand &= ~(1u << (be >> 5));
+        if (lane == k) my_id = be;
+    }
+    return my_id;
+}
+
+// Groups on fp32 choices (key: their images, cleared for the experts of groups that do not stay). Returns whether the choice of groups
+// is certain. Each group is read by 32 / 2^ceil(log2 groups) lanes.
+template <int NPL>
+__device__ __forceinline__ bool pick_groups(const RouteGeneralParams& p, unsigned (&key)[NPL], unsigned* sk, int lane) {
+    const int N = p.N, G = p.n_groups, per = N / G;
+    __syncwarp();
+#pragma unroll
+    for (int q = 0; q < NPL; ++q)
+        if (lane + 32 * q < N) sk[lane + 32 * q] = key[q];
+    __syncwarp();
+    int lanes = 32;
+    while (lanes * G > 32) lanes >>= 1;
+    const int g = lane / lanes;
+    unsigned k1 = 0, k2 = 0;
+    if (g < G)
+        for (int j = lane % lanes; j < per; j += lanes) {
+            const unsigned k = sk[g * per + j];
+            k2 = max(k2, min(k1, k));
+            k1 = max(k1, k);
+        }
+    for (int o = lanes >> 1; o > 0; o >>= 1) {
+        const unsigned a = __shfl_xor_sync(0xffffffffu, k1, o), b = __shfl_xor_sync(0xffffffffu, k2, o);
+        k2 = max(min(k1, a), max(k2, b));
+        k1 = max(k1, a);
+    }
+    if (p.group_top2 && k2 > order32(-INFINITY)) k1 = order32(from_order32(k1) + from_order32(k2));
+    if (g >= G) k1 = 0;
+    int place = 0;
+    for (int o = 0; o < G; ++o) {
+        const unsigned ko = __shfl_sync(0xffffffffu, k1, o * lanes);
+        if (ko > k1 || (ko == k1 && o < g)) ++place;
+    }
+    const bool in = g < G && place < p.top_groups;
+    const unsigned stay = __ballot_sync(0xffffffffu, in);
+    const unsigned last = __reduce_min_sync(0xffffffffu, in ? k1 : 0xffffffffu), next = __reduce_max_sync(0xffffffffu, in ? 0u : k1);
+#pragma unroll
+    for (int q = 0; q < NPL; ++q)
+        if (!((stay >> min(31, (lane + 32 * q) / per * lanes)) & 1u)) key[q] = 0;
+    return !p.by_score || !close_call(from_order32(last), from_order32(next), 2.f * (p.softmax ? kErrSoftmax : kErrSigmoid));
+}
+
+// Descending; neighbours change places only if the second is larger, so equal keys stay in the order of their experts
+template <int NPL>
+__device__ __forceinline__ void sort_keys(unsigned (&key)[NPL], int (&id)[NPL]) {
+#pragma unroll
+    for (int r = 0; r < NPL; ++r)
+#pragma unroll
+        for (int a = r & 1; a + 1 < NPL; a += 2) {
+            const bool swap = key[a + 1] > key[a];
+            const unsigned k = key[a];
+            const int i = id[a];
+            key[a] = swap ? key[a + 1] : k;
+            id[a] = swap ? id[a + 1] : i;
+            key[a + 1] = swap ? k : key[a + 1];
+            id[a + 1] = swap ? i : id[a + 1];
+        }
+}
+
+__global__ void __launch_bounds__(kMaxExperts) clear_load_kernel(int32_t* load, int N) {
+    grid_dep_launch();
+    grid_dep_wait();
+    if ((int)threadIdx.x < N) load[threadIdx.x] = 0;
+}
+
+// SLOTS: lanes per token when the weights are computed, K rounded up to 8, 16 or 32; a warp takes `batch` <= 32 / SLOTS tokens at a time
+template <int NPL, int SLOTS>
+__global__ void __launch_bounds__(kGrThreads) route_general_kernel(const __grid_constant__ RouteGeneralParams p) {
+    extern __shared__ unsigned long long s_key[];  // [warps][N]
+    __shared__ int hist[kMaxExperts];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = (int)blockDim.x >> 5;
+    const int N = p.N, K = p.K, batch = p.batch;
+    unsigned long long* sk = s_key + warp * N;
     grid_dep_launch();
     if (p.load != nullptr) {
-        for (int e = threadIdx.x; e < N; e += kGrThreads) hist[e] = 0;
+        for (int e = threadIdx.x; e < N; e += blockDim.x) hist[e] = 0;
         __syncthreads();
     }
     grid_dep_wait();
-    for (int64_t i = (int64_t)blockIdx.x * kGrWarps + warp; i < p.T; i += (int64_t)gridDim.x * kGrWarps) {
-        const float* z = p.logits + i * N;
+    float bias[NPL];
+#pragma unroll
+    for (int q = 0; q < NPL; ++q) bias[q] = p.bias != nullptr && lane + 32 * q < N ? p.bias[lane + 32 * q] : 0.f;
+    const int64_t step = (int64_t)gridDim.x * warps * batch;
+    for (int64_t i0 = ((int64_t)blockIdx.x * warps + warp) * batch; i0 < p.T; i0 += step) {
+        const int here = (int)min((int64_t)batch, p.T - i0);
+        int my_id = 0;              // lane SLOTS t + k: of token i0 + t, slot k
+        double my_max = 0.0, my_sum = 1.0;  // softmax over all experts: that token's
         float v[NPL];
-        unsigned long long key[NPL];
-        unsigned cand = 0, masked = 0;  // bits of this lane's experts
-        float zmax = -INFINITY;
 #pragma unroll
-        for (int q = 0; q < NPL; ++q) {
-            const int e = lane + 32 * q;
-            v[q] = e < N ? z[e] : -INFINITY;
-            if (e < N) cand |= 1u << q;
-            if (v[q] <= kMaskedScore) masked |= 1u << q;
-            zmax = isnan(v[q]) || v[q] > zmax ? v[q] : zmax;
-        }
-        double sum = 0.0;
-        if (p.softmax) {
-            zmax = float_from_order_key(__reduce_max_sync(0xffffffffu, order32(zmax)));
+        for (int q = 0; q < NPL; ++q) v[q] = lane + 32 * q < N ? p.logits[i0 * N + lane + 32 * q] : -INFINITY;
+        for (int t = 0; t < here; ++t) {
+            const float* z = p.logits + (i0 + t) * N;
+            float next[NPL];  // the next token's scores on their way
 #pragma unroll
-            for (int q = 0; q < NPL; ++q)
-                if (!((masked >> q) & 1u)) sum += exp((double)v[q] - (double)zmax);
+            for (int q = 0; q < NPL; ++q) next[q] = t + 1 < here && lane + 32 * q < N ? z[N + lane + 32 * q] : -INFINITY;
+            unsigned key[NPL];
+            int id[NPL];
+            if (p.softmax && (p.by_score || !p.renormalise)) {
+                float zmax = -INFINITY;
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        }
-        auto score = [&](float zz) -> double {
-            if (zz <= kMaskedScore) return 0.0;
-            return p.softmax ? exp((double)zz - (double)zmax) / sum : 1.0 / (1.0 + exp(-(double)zz));
-        };
+                for (int q = 0; q < NPL; ++q) zmax = isnan(v[q]) || v[q] > zmax ? v[q] : zmax;
+                zmax = from_order32(__reduce_max_sync(0xffffffffu, order32(zmax)));
+                float ex[NPL], sum = 0.f;
+                if (!p.renormalise) {  // the weights are quotients of the whole sum
+                    double part = 0.0;
 #pragma unroll
-        for (int q = 0; q < NPL; ++q) {
-            const int e = lane + 32 * q;
-            const double c = (masked >> q) & 1u ? -INFINITY : p.by_score ? score(v[q]) + (p.bias != nullptr && e < N ? (double)p.bias[e] : 0.0) : (double)v[q];
-            key[q] = order64(c);
-        }
-        if (p.n_groups > 1) {
-            // groups: lane g takes group g's score and its place among the groups
-            unsigned long long* sk = s_key + warp * N;
-            __syncwarp();
+                    for (int q = 0; q < NPL; ++q) {
+                        const double e = v[q] <= kMaskedScore ? 0.0 : exp((double)v[q] - (double)zmax);
+                        part += e;
+                        ex[q] = (float)e;
+                    }
 #pragma unroll
-            for (int q = 0; q < NPL; ++q)
-                if (lane + 32 * q < N) sk[lane + 32 * q] = key[q];
-            __syncwarp();
-            const int per = N / p.n_groups;
-            unsigned long long k1 = 0, k2 = 0;
-            if (lane < p.n_groups)
-                for (int j = 0; j < per; ++j) {
-                    const unsigned long long k = sk[lane * per + j];
-                    if (k > k1) { k2 = k1; k1 = k; }
-                    else if (k > k2) k2 = k;
+                    for (int o = 16; o > 0; o >>= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
+                    sum = (float)part;
+                    if (lane / SLOTS == t) {
+                        my_max = (double)zmax;
+                        my_sum = part;
+                    }
+                } else {
+#pragma unroll
+                    for (int q = 0; q < NPL; ++q) {
+                        ex[q] = v[q] <= kMaskedScore ? 0.f : expf(v[q] - zmax);
+                        sum += ex[q];
+                    }
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
                 }
-            if (p.group_top2) {
-                auto value = [](unsigned long long k) {
-                    if (k == ~0ull) return (double)NAN;
-                    return __longlong_as_double((long long)((k >> 63) ? k & ~(1ull << 63) : ~k));
-                };
-                const unsigned long long none = order64(-INFINITY);
-                if (k2 > none) k1 = order64(value(k1) + value(k2));
-            }
-            int place = 0;
-            for (int g = 0; g < p.n_groups; ++g) {
-                const unsigned long long kg = __shfl_sync(0xffffffffu, k1, g);
-                if (kg > k1 || (kg == k1 && g < lane)) ++place;
-            }
-            const unsigned stay = __ballot_sync(0xffffffffu, lane < p.n_groups && place < p.top_groups);
 #pragma unroll
-            for (int q = 0; q < NPL; ++q)
-                if (!((stay >> min(31, (lane + 32 * q) / per)) & 1u)) cand &= ~(1u << q);
-        }
-        int my_id = 0;
-        for (int k = 0; k < K; ++k) {
-            unsigned long long bk = 0;
-            int be = 0x7fffffff;
+                for (int q = 0; q < NPL; ++q) key[q] = order32(p.by_score ? __fdividef(ex[q], sum) + bias[q] : v[q]);
+            } else {
 #pragma unroll
-            for (int q = 0; q < NPL; ++q)
-                if (((cand >> q) & 1u) && (be == 0x7fffffff || key[q] > bk)) {
-                    bk = key[q];
-                    be = lane + 32 * q;
+                for (int q = 0; q < NPL; ++q)
+                    key[q] = order32(p.by_score ? __fdividef(1.f, 1.f + __expf(v[q] < -80.f ? 80.f : -v[q])) + bias[q] : v[q]);
+            }
+#pragma unroll
+            for (int q = 0; q < NPL; ++q) {
+                if (v[q] <= kMaskedScore) key[q] = order32(-INFINITY);
+                if (lane + 32 * q >= N) key[q] = 0;
+                id[q] = lane + 32 * q;
+            }
+            bool sure = true;
+            if (p.n_groups > 1) sure = pick_groups<NPL>(p, key, reinterpret_cast<unsigned*>(sk), lane);
+            sort_keys<NPL>(key, id);
+            int pick = 0;            // lane k: the k-th
+            unsigned pick_key = 0;
+            const int rounds = p.by_score ? min(K + 1, 32) : K;
+            for (int k = 0; k < rounds; ++k) {
+                const unsigned best = __reduce_max_sync(0xffffffffu, key[0]);
+                const int e = (int)__reduce_min_sync(0xffffffffu, key[0] == best ? (unsigned)id[0] : 0xffffffffu);
+                if (lane == k) {
+                    pick = e;
+                    pick_key = best;
                 }
-            const bool has = be != 0x7fffffff;
-            const unsigned hi = __reduce_max_sync(0xffffffffu, has ? (unsigned)(bk >> 32) : 0u);
-            const bool top = has && (unsigned)(bk >> 32) == hi;
-            const unsigned lo = __reduce_max_sync(0xffffffffu, top ? (unsigned)bk : 0u);
-            be = __reduce_min_sync(0xffffffffu, top && (unsigned)bk == lo ? be : 0x7fffffff);
-            if ((be & 31) == lane) cand &= ~(1u << (be >> 5));
-            if (lane == k) my_id = be;
+                if (e == id[0]) {
+#pragma unroll
+                    for (int q = 0; q + 1 < NPL; ++q) {
+                        key[q] = key[q + 1];
+                        id[q] = id[q + 1];
+                    }
+                    key[NPL - 1] = 0;
+                    id[NPL - 1] = -1;
+                }
+            }
+            if (p.by_score) {
+                const float err = p.softmax ? kErrSoftmax : kErrSigmoid, c = from_order32(pick_key), before = __shfl_up_sync(0xffffffffu, c, 1);
+                // (a key of 0 is no expert: there are no more)
+                const unsigned close = __ballot_sync(0xffffffffu, lane > 0 && lane < rounds && pick_key != 0 && close_call(before, c, err));
+                if (close != 0 || !sure || rounds == K) {  // warp-uniform
+                    const unsigned more = __reduce_max_sync(0xffffffffu, key[0]);
+                    // the set is open: its last one is as close to the next as may be
+                    const bool open = (rounds == K || ((close >> K) & 1u)) && more != 0 &&
+                                      close_call(__shfl_sync(0xffffffffu, c, rounds - 1), from_order32(more), err);
+                    if (p.softmax || !sure || open) pick = pick_exact<NPL>(p, z, sk, lane);
+                    else if (close != 0) pick = rank_exact(p, z, pick, __popc(__ballot_sync(0xffffffffu, pick_key != 0)), lane);
+                }
+            }
+            const int mine = __shfl_sync(0xffffffffu, pick, lane % SLOTS);
+            if (lane / SLOTS == t) my_id = mine;
+#pragma unroll
+            for (int q = 0; q < NPL; ++q) v[q] = next[q];
         }
-        double s = lane < K ? score(z[my_id]) : 0.0;
+        // weights of all tokens of the batch
+        const int t = lane / SLOTS, k = lane % SLOTS;
+        const bool slot = t < here && k < K;
+        const int64_t i = i0 + t;
+        const float zk = slot ? p.logits[i * N + my_id] : -INFINITY;
+        const bool live = slot && !(zk <= kMaskedScore);
+        double s = 0.0;
+        if (!p.softmax) {
+            if (live) s = 1.0 / (1.0 + exp(-(double)zk));
+        } else if (p.renormalise) {
+            unsigned m = order32(live ? zk : -INFINITY);
+#pragma unroll
+            for (int o = SLOTS / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+            if (live) s = exp((double)zk - (double)from_order32(m));
+        } else if (live) {
+            s = exp((double)zk - my_max) / my_sum;
+        }
         if (p.renormalise) {
-            double total = 0.0;
-            for (int k = 0; k < K; ++k) total += __shfl_sync(0xffffffffu, s, k);
+            double total = s;
+#pragma unroll
+            for (int o = SLOTS / 2; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
             s = total != 0.0 ? s / total : 0.0;
         }
-        if (lane < K) {
-            p.ids[i * K + lane] = my_id;
-            p.w[i * K + lane] = (float)(s * (double)p.scale);
+        if (slot) {
+            p.ids[i * K + k] = my_id;
+            p.w[i * K + k] = (float)(s * (double)p.scale);
             if (p.load != nullptr) atomicAdd(&hist[my_id], 1);
         }
     }
-    if (p.load != nullptr) {
-        __syncthreads();
-        for (int e = threadIdx.x; e < N; e += kGrThreads) {
-            if (gridDim.x == 1) p.load[e] = hist[e];
-            else if (hist[e] != 0) atomicAdd(&p.load[e], hist[e]);
-        }
+    if (p.load == nullptr) return;
+    __syncthreads();
+    for (int e = threadIdx.x; e < N; e += blockDim.x) {
+        if (gridDim.x == 1) p.load[e] = hist[e];
+        else if (hist[e] != 0) atomicAdd(&p.load[e], hist[e]);
     }
 }
 
 // One warp per token: lane k < K holds the chosen expert k, the row is put together in registers
 template <int NPL>
 __global__ void __launch_bounds__(kGrThreads) route_backward_kernel(RouteBackwardParams p) {
+    constexpr int kWarps = kGrThreads / 32;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int N = p.N, K = p.K;
     grid_dep_launch();
     grid_dep_wait();
-    for (int64_t i = (int64_t)blockIdx.x * kGrWarps + warp; i < p.T; i += (int64_t)gridDim.x * kGrWarps) {
+    for (int64_t i = (int64_t)blockIdx.x * kWarps + warp; i < p.T; i += (int64_t)gridDim.x * kWarps) {
         const float* z = p.logits + i * N;
         const bool dense = p.softmax && !p.renormalise;
         float out[NPL];
@@ -168,7 +396,7 @@ __global__ void __launch_bounds__(kGrThreads) route_backward_kernel(RouteBackwar
                 v[q] = lane + 32 * q < N ? z[lane + 32 * q] : -INFINITY;
                 zmax = isnan(v[q]) || v[q] > zmax ? v[q] : zmax;
             }
-            zmax = float_from_order_key(__reduce_max_sync(0xffffffffu, order32(zmax)));
+            zmax = from_order32(__reduce_max_sync(0xffffffffu, order32(zmax)));
             float sum = 0.f;
 #pragma unroll
             for (int q = 0; q < NPL; ++q) {
@@ -187,7 +415,7 @@ __global__ void __launch_bounds__(kGrThreads) route_backward_kernel(RouteBackwar
         } else {
             double s = 0.0, rest = 1.0;  // score (softmax: up to a factor), 1 - score
             if (p.softmax) {
-                const float m = float_from_order_key(__reduce_max_sync(0xffffffffu, order32(live ? zk : -INFINITY)));
+                const float m = from_order32(__reduce_max_sync(0xffffffffu, order32(live ? zk : -INFINITY)));
                 if (live) s = exp((double)zk - (double)m);
             } else if (live) {
                 const double e = exp(-fabs((double)zk)), r = 1.0 / (1.0 + e);
@@ -226,25 +454,36 @@ __global__ void __launch_bounds__(kGrThreads) route_backward_kernel(RouteBackwar
 
 }  // namespace
 
-cudaError_t launch_route_general(const RouteGeneralParams& p, int sms, cudaStream_t s) {
-    const unsigned blocks = (unsigned)std::max<int64_t>(1, std::min<int64_t>((p.T + kGrWarps - 1) / kGrWarps, (int64_t)8 * sms));
+cudaError_t launch_route_general(RouteGeneralParams p, int sms, cudaStream_t s) {
+    constexpr int kWarps = kGrThreads / 32;
+    const int slots = p.K <= 8 ? 8 : p.K <= 16 ? 16 : 32;
+    // Long prompts: several tokens of a warp share the 64-bit part; short ones take a warp each, it is one token's chain of latencies then
+    p.batch = p.T >= (int64_t)sms * kWarps * 4 ? 32 / slots : 1;
+    const unsigned blocks = (unsigned)std::max<int64_t>(1, std::min<int64_t>((p.T + kWarps * p.batch - 1) / (kWarps * p.batch), (int64_t)8 * sms));
+    // load: several CTAs add theirs up in memory, which a kernel clears first (a memset, which the next kernel cannot be launched under,
+    // took 3.5 us of a call; CTAs of a cluster that add up between themselves, for 64 tokens, 0.9 us more than this)
     if (p.load != nullptr && (blocks > 1 || p.T == 0)) {
-        cudaError_t e = cudaMemsetAsync(p.load, 0, (size_t)p.N * sizeof(int32_t), s);
+        cudaError_t e = launch_pdl(clear_load_kernel, 1, kMaxExperts, 0, s, p.load, p.N);
         if (e != cudaSuccess) return e;
     }
     if (p.T == 0) return cudaSuccess;
-    const size_t smem = p.n_groups > 1 ? (size_t)kGrWarps * p.N * sizeof(unsigned long long) : 0;
+    const size_t smem = p.n_groups > 1 ? (size_t)kWarps * p.N * sizeof(unsigned long long) : 0;
+    auto go = [&](auto kernel) { return launch_pdl(kernel, blocks, kGrThreads, smem, s, p); };
+#define EXFOLD_ROUTE(NPL) \
+    return slots == 8 ? go(route_general_kernel<NPL, 8>) : slots == 16 ? go(route_general_kernel<NPL, 16>) : go(route_general_kernel<NPL, 32>)
     switch ((p.N + 31) / 32) {
-        case 1: return launch_pdl(route_general_kernel<1>, blocks, kGrThreads, smem, s, p);
-        case 2: return launch_pdl(route_general_kernel<2>, blocks, kGrThreads, smem, s, p);
-        case 3: case 4: return launch_pdl(route_general_kernel<4>, blocks, kGrThreads, smem, s, p);
-        default: return launch_pdl(route_general_kernel<8>, blocks, kGrThreads, smem, s, p);
+        case 1: EXFOLD_ROUTE(1);
+        case 2: EXFOLD_ROUTE(2);
+        case 3: case 4: EXFOLD_ROUTE(4);
+        default: EXFOLD_ROUTE(8);
     }
+#undef EXFOLD_ROUTE
 }
 
 cudaError_t launch_route_backward(const RouteBackwardParams& p, int sms, cudaStream_t s) {
     if (p.T == 0) return cudaSuccess;
-    const unsigned blocks = (unsigned)std::min<int64_t>((p.T + kGrWarps - 1) / kGrWarps, (int64_t)8 * sms);
+    constexpr int kWarps = kGrThreads / 32;
+    const unsigned blocks = (unsigned)std::min<int64_t>((p.T + kWarps - 1) / kWarps, (int64_t)8 * sms);
     switch ((p.N + 31) / 32) {
         case 1: return launch_pdl(route_backward_kernel<1>, blocks, kGrThreads, 0, s, p);
         case 2: return launch_pdl(route_backward_kernel<2>, blocks, kGrThreads, 0, s, p);
