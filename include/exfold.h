@@ -328,7 +328,7 @@ int exfold_route(const exfold_layer *layer, const float *logits, int64_t T, cons
 /*
  * Gradient of exfold_route's weights for tuning a router: dw [T][K] = dLoss/dw -> dlogits [T][N] = dLoss/dlogits, every
  * element written. The choice is a constant, so the bias and the groups play no part (`router` gives score, renormalise
- * and scale). ids as exfold_route wrote them; an id outside [0, N) has no gradient. With g = dw, p_k = s_k / sum_j s_j and
+ * and scale). ids as exfold_route wrote them (a token's are different ones); an id outside [0, N) has no gradient. With g = dw, p_k = s_k / sum_j s_j and
  * gm = sum_j g_j p_j over the chosen:
  *     renormalised      softmax scale p_k (g_k - gm), sigmoid the same times (1 - s_k); 0 for the other experts
  *     not renormalised  sigmoid scale g_k s_k (1 - s_k), 0 for the others; softmax scale s_e ([e chosen] g_e - sum_k g_k s_k)

@@ -186,7 +186,7 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 def _stream(stream: Optional[torch.cuda.Stream]) -> int:
     # the raw handle of the current stream: torch.cuda.current_stream() builds a Stream object first, 3.3 us per call
-    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def make_layer(n_experts: int, n_shared: int, hidden: int, inter: int, top_k: int, dtype) -> exfold_layer:
@@ -425,17 +425,19 @@ def make_router(score: str = "softmax", bias: Optional[torch.Tensor] = None, n_g
 
 
 def _typed(t: Optional[torch.Tensor], dtype, shape) -> Optional[int]:
-    if t is not None:
-        assert t.dtype == dtype and t.shape == shape, f"expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}"
-    return _ptr(t)
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise AssertionError(f"expected contiguous {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)} {t.stride()}")
+    return t.data_ptr()
 
 
 def exfold_route(layer, logits, router: exfold_router, ids, w, load=None, stream=None, check: bool = True) -> int:
     """logits [T][N] fp32 -> ids [T][K] int32, w [T][K] fp32, load [N] int32 (tokens per expert)."""
     T, N, K = logits.shape[0], layer.n_experts, layer.top_k
-    rc = lib.exfold_route(C.byref(layer), _typed(logits, torch.float32, (T, N)), T, C.byref(router),
-                          _typed(ids, torch.int32, (T, K)), _typed(w, torch.float32, (T, K)),
-                          _typed(load, torch.int32, (N,)), _stream(stream))
+    rc = lib.exfold_route(layer, _typed(logits, torch.float32, (T, N)), T, router, _typed(ids, torch.int32, (T, K)),
+                          _typed(w, torch.float32, (T, K)), _typed(load, torch.int32, (N,)) if load is not None else None,
+                          _stream(stream))
     if check and rc != 0:
         raise ExfoldError(rc, "exfold_route")
     return rc
@@ -444,9 +446,9 @@ def exfold_route(layer, logits, router: exfold_router, ids, w, load=None, stream
 def exfold_route_backward(layer, logits, ids, dw, router: exfold_router, dlogits, stream=None, check: bool = True) -> int:
     """dw [T][K], the gradient of exfold_route's weights -> dlogits [T][N]."""
     T, N, K = logits.shape[0], layer.n_experts, layer.top_k
-    rc = lib.exfold_route_backward(C.byref(layer), _typed(logits, torch.float32, (T, N)), _typed(ids, torch.int32, (T, K)),
-                                   _typed(dw, torch.float32, (T, K)), T, C.byref(router),
-                                   _typed(dlogits, torch.float32, (T, N)), _stream(stream))
+    rc = lib.exfold_route_backward(layer, _typed(logits, torch.float32, (T, N)), _typed(ids, torch.int32, (T, K)),
+                                   _typed(dw, torch.float32, (T, K)), T, router, _typed(dlogits, torch.float32, (T, N)),
+                                   _stream(stream))
     if check and rc != 0:
         raise ExfoldError(rc, "exfold_route_backward")
     return rc
@@ -517,12 +519,16 @@ def exfold_linear(x, w, y, ws, bias=None, residual=None, activation: str = "none
     """y = act(x w^T + bias) + residual. x [T][in], w [out][in], bias [out] of one type; y, residual [T][out]. The matrices may
     have any distance between their rows."""
     T, i = x.shape
-    o, dt, out = w.shape[0], x.dtype, y.dtype
-    desc = _linear_desc(i, o, _LINEAR_DTYPES[dt], _LINEAR_DTYPES[out], ACTIVATIONS[activation], _rows(x, dt, T, i),
-                        _rows(w, dt, o, i), _rows(y, out, T, o), _rows(residual, out, T, o) if residual is not None else 0)
-    if bias is not None:
-        assert bias.dtype == dt and bias.shape == (o,) and bias.is_contiguous(), f"expected bias {dt} {(o,)}"
-    rc = lib.exfold_linear(desc, x.data_ptr(), w.data_ptr(), bias.data_ptr() if bias is not None else None,
+    o, dt, out, ldr = w.shape[0], x.dtype, y.dtype, 0
+    (ldx, sx), (ldw, sw), (ldy, sy) = x.stride(), w.stride(), y.stride()
+    if not (sx == sw == sy == 1 and ldx >= i and ldw >= i and ldy >= o and w.shape[1] == i and w.dtype is dt and y.shape == (T, o)):
+        ldx, ldw, ldy = _rows(x, dt, T, i), _rows(w, dt, o, i), _rows(y, out, T, o)  # matrices of one row or column, or not usable
+    if residual is not None:
+        ldr = _rows(residual, out, T, o)
+    if bias is not None and (bias.dtype is not dt or bias.shape != (o,) or not bias.is_contiguous()):
+        raise AssertionError(f"expected bias {dt} {(o,)}, got {bias.dtype} {tuple(bias.shape)}")
+    rc = lib.exfold_linear(_linear_desc(i, o, _LINEAR_DTYPES[dt], _LINEAR_DTYPES[out], ACTIVATIONS[activation], ldx, ldw, ldy, ldr),
+                           x.data_ptr(), w.data_ptr(), bias.data_ptr() if bias is not None else None,
                            residual.data_ptr() if residual is not None else None, T, y.data_ptr(), ws.data_ptr(), ws.numel(),
                            _stream(stream))
     if check and rc != 0:

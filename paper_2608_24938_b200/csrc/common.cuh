@@ -260,9 +260,10 @@ struct RouteBackwardParams {
     int N, K, softmax, renormalise;
     float scale;
     float* dlogits;  // [T][N]
+    int batch;       // set by the launcher
 };
 cudaError_t launch_route_general(RouteGeneralParams p, int sms, cudaStream_t s);
-cudaError_t launch_route_backward(const RouteBackwardParams& p, int sms, cudaStream_t s);
+cudaError_t launch_route_backward(RouteBackwardParams p, int sms, cudaStream_t s);
 
 // ---------------------------------------------------------------- routing (decode)
 struct DecodeRouteParams {

@@ -144,7 +144,7 @@ struct LinearReduce {
 };
 template <int S, typename O, int THREADS, typename B>
 struct LinearReduce<S, O, THREADS, false, B> {
-    static constexpr int U = S >= 8 ? 2 : S == 4 ? 4 : 8, kStride = S * THREADS;
+    static constexpr int U = S >= 8 ? 2 : S >= 3 ? 4 : 8, kStride = S * THREADS;
     const LinearParams& l;
     int shift, total, n0, i0;
     int64_t row0;

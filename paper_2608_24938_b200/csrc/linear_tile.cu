@@ -1,5 +1,5 @@
-// Dense product with epilogue, bf16 operands, few tokens or few tiles: one CTA per 128 tokens x bn features, K split over a
-// cluster.
+// Dense product with epilogue, bf16 operands, few tokens or few tiles: one CTA per 128 tokens (or fewer, all tiles alike) x bn features,
+// K split over a cluster.
 //
 // A decode batch reads the whole weight matrix for a few tokens, so its time is the weights' bytes over HBM and what a launch
 // costs; a short prompt has fewer 256 x 256 tiles than SM pairs. Either way the work has to be spread over K: a cluster of `split`
@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(kLtThreads, 2) linear_tile_kernel(const __grid
     const int bn = p.plan.bn, stages = p.plan.stages, rank = (int)cluster.block_rank();
     const int nt = (p.l.N + bn - 1) / bn, tile = (int)blockIdx.x / split;
     const int n0 = tile % nt * bn;
-    const int64_t row0 = (int64_t)(tile / nt) * kTileM;
+    const int64_t row0 = (int64_t)(tile / nt) * p.plan.a_rows;
     uint32_t tmem_cols = 32;
     while ((int)tmem_cols < bn) tmem_cols *= 2;
     if (threadIdx.x == 0) {
@@ -72,7 +72,7 @@ __global__ void __launch_bounds__(kLtThreads, 2) linear_tile_kernel(const __grid
     const int nkb = (p.l.K + kLtBK - 1) / kLtBK;
     const int kb0 = rank * nkb / split, kb1 = (rank + 1) * nkb / split;  // never empty: split <= nkb
     const int a_bytes = p.plan.a_rows * kLtBK * 2, stage_bytes = a_bytes + bn * kLtBK * 2;
-    const int rows = (int)min((int64_t)kTileM, p.l.T - row0);
+    const int rows = (int)min((int64_t)p.plan.a_rows, p.l.T - row0);
     const int part_ld = bn + 4;  // floats: 16-byte aligned rows, the rows of a quarter warp in distinct banks
     const LinearEpilogue<O> ep(p.l);
     LinearReduce<SPLIT, O, 32 * kLtEpiWarps, WHOLE> reduce(ep, rows, bn, row0, n0, rank, (int)threadIdx.x - 64);
@@ -152,23 +152,28 @@ __global__ void __launch_bounds__(kLtThreads, 2) linear_tile_kernel(const __grid
 
 }  // namespace
 
-// 64 features per tile, and K split while two CTAs per SM have room for the parts and a part has four k-blocks. Where 64 features leave
-// no room to split, 128 and a split in two take less operand traffic. On the GPU, with bias and residual, 64 features / 128 in two:
-// 64 x 14336 x 4096 (tokens x features x K) 25.9 / 24.6 us, 128 x 14336 x 4096 31.7 / 28.4, 512 x 4096 x 4096 26.9 / 23.3; the other way
+// Row tiles alike, as few as 128 rows allow. 64 features per tile; where their tiles leave no room to split, 128 and a split take less
+// operand traffic. K is split while two CTAs per SM have room for the parts (one alone takes in 73 KB per us, two 110) and a part has four
+// k-blocks; in three where that leaves the SMs better balanced than two or four. On the GPU, with bias and residual, 64 features / 128 in
+// two: 64 x 14336 x 4096 (tokens x features x K) 25.9 / 24.6 us, 128 x 14336 x 4096 31.7 / 28.4, 512 x 4096 x 4096 26.9 / 23.3; the other way
 // 64 x 4096 x 4096 in 64 x 4 parts / 128 x 2 11.0 / 13.1, 256 x 4096 x 4096 16.9 / 20.1, 1024 x 2048 x 768 10.8 / 12.1.
 LinearTilePlan linear_tile_plan(int64_t T, int N, int K, int sms) {
     LinearTilePlan q{};
-    q.a_rows = (int)std::min<int64_t>(kTileM, (T + 15) / 16 * 16);
+    const int64_t mt = (T + kTileM - 1) / kTileM;
+    q.a_rows = (int)(((T + mt - 1) / mt + 15) / 16 * 16);
     const int nkb = (K + kLtBK - 1) / kLtBK;
     q.bn = N <= 32 ? 32 : 64;
-    int64_t tiles = (T + kTileM - 1) / kTileM * ((N + q.bn - 1) / q.bn);
-    q.split = 1;
-    const int64_t wide = (T + kTileM - 1) / kTileM * ((N + 127) / 128);
+    int64_t tiles = mt * ((N + q.bn - 1) / q.bn);
+    const int64_t wide = mt * ((N + 127) / 128);
     if (tiles > sms && wide <= sms && nkb >= 16) {
         q.bn = 128;
         tiles = wide;
     }
+    // k-blocks that the SM with the most of them gets
+    auto most = [&](int split) { return (tiles * split + sms - 1) / sms * ((nkb + split - 1) / split); };
+    q.split = 1;
     while (q.split < 8 && tiles * q.split <= sms && nkb >= 8 * q.split) q.split *= 2;
+    if ((q.split == 2 || q.split == 4) && tiles * 3 <= 2 * sms && nkb >= 12 && most(3) < most(q.split)) q.split = 3;
     const int stage_bytes = (q.a_rows + q.bn) * kLtBK * 2;
     const int per = (nkb + q.split - 1) / q.split;
     q.stages = std::max(2, std::min(std::min(kLtMaxStages, per), 104 * 1024 / stage_bytes));
@@ -196,17 +201,18 @@ bool linear_prefers_pairs(int64_t T, int N, int K, int sms) {
 
 cudaError_t launch_linear_tile(const LinearTileParams& p, bool out_bf16, cudaStream_t s) {
     const LinearTilePlan& q = p.plan;
-    const int64_t grid = (p.l.T + kTileM - 1) / kTileM * ((p.l.N + q.bn - 1) / q.bn) * q.split;
+    const int64_t grid = (p.l.T + q.a_rows - 1) / q.a_rows * ((p.l.N + q.bn - 1) / q.bn) * q.split;
     if (grid > 0x7fffffff) return cudaErrorInvalidValue;
     auto go = [&](auto kernel) {
         const cudaError_t e = ensure_smem(kernel, q.smem);
         return e != cudaSuccess ? e : launch_pdl_cluster(kernel, (unsigned)grid, kLtThreads, q.smem, q.split, s, p);
     };
-    auto pick = [&](auto one, auto two, auto four, auto eight) {
-        return q.split == 1 ? go(one) : q.split == 2 ? go(two) : q.split == 4 ? go(four) : go(eight);
+    auto pick = [&](auto one, auto two, auto three, auto four, auto eight) {
+        return q.split == 1 ? go(one) : q.split == 2 ? go(two) : q.split == 3 ? go(three) : q.split == 4 ? go(four) : go(eight);
     };
     const bool whole = out_bf16 ? LinearEpilogue<__nv_bfloat16>(p.l).whole() : LinearEpilogue<float>(p.l).whole();
-#define EXFOLD_LT(O, W) pick(linear_tile_kernel<O, 1, W>, linear_tile_kernel<O, 2, W>, linear_tile_kernel<O, 4, W>, linear_tile_kernel<O, 8, W>)
+#define EXFOLD_LT(O, W) \
+    pick(linear_tile_kernel<O, 1, W>, linear_tile_kernel<O, 2, W>, linear_tile_kernel<O, 3, W>, linear_tile_kernel<O, 4, W>, linear_tile_kernel<O, 8, W>)
     if (out_bf16) return whole ? EXFOLD_LT(__nv_bfloat16, true) : EXFOLD_LT(__nv_bfloat16, false);
     return whole ? EXFOLD_LT(float, true) : EXFOLD_LT(float, false);
 #undef EXFOLD_LT

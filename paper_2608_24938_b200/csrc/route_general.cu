@@ -17,7 +17,9 @@
 // s (1 - s) times: below 1.3; the sum 1, the quotient 4. Softmax: the argument's rounding counts d e^-d <= 0.4, expf 4, the sum 13, the
 // quotient 4: below 22. And the addition's half step of the choice. Two choices are sure of their order if further apart than twice that.
 //
-// GPU time, 64-bit choices for every token -> now: 16384 tokens x 128 experts 23.2 -> KKK us.
+// GPU time, 64-bit choices for every token -> now (sigmoid, bias, Top-8): 16384 tokens x 128 experts 23.2 -> 12.7 us, 777 x 256 in 8 groups
+// with the load 13.2 -> 6.3, one token 4.4 -> 2.5; gradient, a token per warp -> now: 16384 x 128 13.0 -> 3.8, softmax over all experts 6.9.
+// Ranking by one word (24 bits of the choice, 8 of the expert: one reduction per round instead of two) took 12.1 and 6.9 us.
 #include <algorithm>
 
 #include "common.cuh"
@@ -49,7 +51,7 @@ __device__ __forceinline__ bool close_call(float a, float b, float err) {
 }
 
 // `n` experts, one per lane, in the order of 64-bit choices (sigmoid scores): lane k returns the k-th
-__device__ __noinline__ int rank_exact(const RouteGeneralParams& p, const float* z, int id, int n, int lane) {
+__device__ __forceinline__ int rank_exact(const RouteGeneralParams& p, const float* z, int id, int n, int lane) {
     unsigned long long key = 0;
     if (lane < n) {
         const float v = z[id];
@@ -72,7 +74,7 @@ __device__ __noinline__ int rank_exact(const RouteGeneralParams& p, const float*
 
 // One token's experts from 64-bit choices: lane k < K returns the k-th. cand: this lane's experts; sk: scratch of N words of the warp.
 template <int NPL>
-__device__ __noinline__ int pick_exact(const RouteGeneralParams& p, const float* z, unsigned long long* sk, int lane) {
+__device__ __forceinline__ int pick_exact(const RouteGeneralParams& p, const float* z, unsigned long long* sk, int lane) {
     const int N = p.N, K = p.K;
     unsigned long long key[NPL];
     unsigned cand = 0;
@@ -369,54 +371,83 @@ __global__ void __launch_bounds__(kGrThreads) route_general_kernel(const __grid_
     }
 }
 
-// One warp per token: lane k < K holds the chosen expert k, the row is put together in registers
-template <int NPL>
-__global__ void __launch_bounds__(kGrThreads) route_backward_kernel(RouteBackwardParams p) {
-    constexpr int kWarps = kGrThreads / 32;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int N = p.N, K = p.K;
+// The gradient, up to `batch` <= 32 / SLOTS tokens of a warp at a time: lane SLOTS t + k holds token t's chosen expert k. Rows are written
+// without the chosen ones (zeros, or the softmax over all experts), and those after them. VEC: rows of whole, aligned groups of four,
+// expert 4 lane + j + 128 q in v[q][j]; else expert lane + 32 (4 q + j). A row is 4 N bytes written, and as many read where the softmax is
+// over all experts.
+template <int NQ, int SLOTS, bool VEC>
+__global__ void __launch_bounds__(kGrThreads) route_backward_kernel(const __grid_constant__ RouteBackwardParams p) {
+    constexpr int kBatch = 32 / SLOTS;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = (int)blockDim.x >> 5;
+    const int N = p.N, K = p.K, batch = p.batch;
+    const bool dense = p.softmax && !p.renormalise;
+    auto expert = [&](int q, int j) { return VEC ? 4 * lane + 128 * q + j : lane + 32 * (4 * q + j); };
     grid_dep_launch();
     grid_dep_wait();
-    for (int64_t i = (int64_t)blockIdx.x * kWarps + warp; i < p.T; i += (int64_t)gridDim.x * kWarps) {
-        const float* z = p.logits + i * N;
-        const bool dense = p.softmax && !p.renormalise;
-        float out[NPL];
-#pragma unroll
-        for (int q = 0; q < NPL; ++q) out[q] = 0.f;
-        int id = lane < K ? p.ids[i * K + lane] : -1;
-        if (id < 0 || id >= N) id = -1;
-        const float g = id >= 0 ? p.dw[i * K + lane] : 0.f;
-        const float zk = id >= 0 ? z[id] : -INFINITY;
+    const int64_t step = (int64_t)gridDim.x * warps * batch;
+    for (int64_t i0 = ((int64_t)blockIdx.x * warps + warp) * batch; i0 < p.T; i0 += step) {
+        const int here = (int)min((int64_t)batch, p.T - i0);
+        const int t = lane / SLOTS, k = lane % SLOTS;
+        const int64_t i = i0 + t;
+        int id = t < here && k < K ? p.ids[i * K + k] : -1;
+        if (id >= N) id = -1;
+        const float g = id >= 0 ? p.dw[i * K + k] : 0.f;
+        const float zk = id >= 0 ? p.logits[i * N + id] : -INFINITY;
         const bool live = zk > kMaskedScore || isnan(zk);
-        float dz;  // of the chosen expert
+        float ex[kBatch][NQ][4];  // softmax over all experts: exp(z - max) of each token's experts
+        float my_max = 0.f, my_inv = 1.f, invs[kBatch];
         if (dense) {
-            float v[NPL], zmax = -INFINITY;
 #pragma unroll
-            for (int q = 0; q < NPL; ++q) {
-                v[q] = lane + 32 * q < N ? z[lane + 32 * q] : -INFINITY;
-                zmax = isnan(v[q]) || v[q] > zmax ? v[q] : zmax;
+            for (int u = 0; u < kBatch; ++u) {
+                if (u >= here) break;
+                const float* z = p.logits + (i0 + u) * N;
+                float zmax = -INFINITY;
+#pragma unroll
+                for (int q = 0; q < NQ; ++q) {
+                    if (VEC) {
+                        float4 w = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+                        if (expert(q, 0) < N) w = *reinterpret_cast<const float4*>(z + expert(q, 0));
+                        ex[u][q][0] = w.x; ex[u][q][1] = w.y; ex[u][q][2] = w.z; ex[u][q][3] = w.w;
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) ex[u][q][j] = expert(q, j) < N ? z[expert(q, j)] : -INFINITY;
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) zmax = isnan(ex[u][q][j]) || ex[u][q][j] > zmax ? ex[u][q][j] : zmax;
+                }
+                zmax = from_order32(__reduce_max_sync(0xffffffffu, order32(zmax)));
+                float sum = 0.f;
+#pragma unroll
+                for (int q = 0; q < NQ; ++q)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        ex[u][q][j] = ex[u][q][j] <= kMaskedScore ? 0.f : expf(ex[u][q][j] - zmax);
+                        sum += ex[u][q][j];
+                    }
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                invs[u] = 1.f / sum;
+                if (t == u) {
+                    my_max = zmax;
+                    my_inv = invs[u];
+                }
             }
-            zmax = from_order32(__reduce_max_sync(0xffffffffu, order32(zmax)));
-            float sum = 0.f;
-#pragma unroll
-            for (int q = 0; q < NPL; ++q) {
-                out[q] = v[q] <= kMaskedScore ? 0.f : expf(v[q] - zmax);
-                sum += out[q];
-            }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            const float sk = live ? expf(zk - zmax) / sum : 0.f;
+        }
+        float dz, dot = 0.f;  // of the chosen expert; dense: sum of the token's
+        if (dense) {
+            const float sk = live ? expf(zk - my_max) * my_inv : 0.f;
             dz = live ? p.scale * g * sk : 0.f;
-            float dot = dz;
+            dot = dz;
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-#pragma unroll
-            for (int q = 0; q < NPL; ++q) out[q] = out[q] == 0.f ? 0.f : -dot * (out[q] / sum);
+            for (int o = SLOTS / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+            dz = live ? dz - dot * sk : 0.f;
         } else {
             double s = 0.0, rest = 1.0;  // score (softmax: up to a factor), 1 - score
             if (p.softmax) {
-                const float m = from_order32(__reduce_max_sync(0xffffffffu, order32(live ? zk : -INFINITY)));
-                if (live) s = exp((double)zk - (double)m);
+                unsigned m = order32(live ? zk : -INFINITY);
+#pragma unroll
+                for (int o = SLOTS / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+                if (live) s = exp((double)zk - (double)from_order32(m));
             } else if (live) {
                 const double e = exp(-fabs((double)zk)), r = 1.0 / (1.0 + e);
                 s = zk >= 0.f ? r : e * r;
@@ -426,29 +457,39 @@ __global__ void __launch_bounds__(kGrThreads) route_backward_kernel(RouteBackwar
             double ds = (double)g;
             double factor = s;
             if (p.renormalise) {
-                double total = s, dot = live ? s * (double)g : 0.0;
+                double total = s, part = live ? s * (double)g : 0.0;
 #pragma unroll
-                for (int o = 16; o > 0; o >>= 1) {
+                for (int o = SLOTS / 2; o > 0; o >>= 1) {
                     total += __shfl_xor_sync(0xffffffffu, total, o);
-                    dot += __shfl_xor_sync(0xffffffffu, dot, o);
+                    part += __shfl_xor_sync(0xffffffffu, part, o);
                 }
-                factor = total != 0.0 ? s / total : 0.0;
-                ds = total != 0.0 ? (double)g - dot / total : 0.0;
+                const double inv = total != 0.0 ? 1.0 / total : 0.0;
+                factor = s * inv;
+                ds = total != 0.0 ? (double)g - part * inv : 0.0;
             }
             dz = live ? (float)((double)p.scale * factor * ds * rest) : 0.f;
         }
-        for (int k = 0; k < K; ++k) {
-            const int e = __shfl_sync(0xffffffffu, id, k);
-            const float d = __shfl_sync(0xffffffffu, dz, k);
-            if (e < 0 || (e & 31) != lane) continue;
 #pragma unroll
-            for (int q = 0; q < NPL; ++q)
-                if (q == (e >> 5)) out[q] += d;
+        for (int u = 0; u < kBatch; ++u) {
+            if (u >= here) break;
+            const float f = dense ? -__shfl_sync(0xffffffffu, dot, SLOTS * u) * invs[u] : 0.f;
+            float* dst = p.dlogits + (i0 + u) * N;
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) {
+                float o[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[j] = dense && ex[u][q][j] != 0.f ? f * ex[u][q][j] : 0.f;  // a masked expert has none
+                if (VEC) {
+                    if (expert(q, 0) < N) *reinterpret_cast<float4*>(dst + expert(q, 0)) = make_float4(o[0], o[1], o[2], o[3]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (expert(q, j) < N) dst[expert(q, j)] = o[j];
+                }
+            }
         }
-        float* dst = p.dlogits + i * N;
-#pragma unroll
-        for (int q = 0; q < NPL; ++q)
-            if (lane + 32 * q < N) dst[lane + 32 * q] = out[q];
+        __syncwarp();
+        if (id >= 0) p.dlogits[i * N + id] = dz;
     }
 }
 
@@ -480,16 +521,19 @@ cudaError_t launch_route_general(RouteGeneralParams p, int sms, cudaStream_t s) 
 #undef EXFOLD_ROUTE
 }
 
-cudaError_t launch_route_backward(const RouteBackwardParams& p, int sms, cudaStream_t s) {
+cudaError_t launch_route_backward(RouteBackwardParams p, int sms, cudaStream_t s) {
     if (p.T == 0) return cudaSuccess;
     constexpr int kWarps = kGrThreads / 32;
-    const unsigned blocks = (unsigned)std::min<int64_t>((p.T + kWarps - 1) / kWarps, (int64_t)8 * sms);
-    switch ((p.N + 31) / 32) {
-        case 1: return launch_pdl(route_backward_kernel<1>, blocks, kGrThreads, 0, s, p);
-        case 2: return launch_pdl(route_backward_kernel<2>, blocks, kGrThreads, 0, s, p);
-        case 3: case 4: return launch_pdl(route_backward_kernel<4>, blocks, kGrThreads, 0, s, p);
-        default: return launch_pdl(route_backward_kernel<8>, blocks, kGrThreads, 0, s, p);
-    }
+    const int slots = p.K <= 8 ? 8 : p.K <= 16 ? 16 : 32;
+    p.batch = p.T >= (int64_t)sms * kWarps * 4 ? 32 / slots : 1;
+    const unsigned blocks = (unsigned)std::min<int64_t>((p.T + kWarps * p.batch - 1) / (kWarps * p.batch), (int64_t)8 * sms);
+    const bool vec = p.N % 4 == 0 && ((reinterpret_cast<uintptr_t>(p.logits) | reinterpret_cast<uintptr_t>(p.dlogits)) & 15) == 0;
+    auto go = [&](auto kernel) { return launch_pdl(kernel, blocks, kGrThreads, 0, s, p); };
+#define EXFOLD_BACK(NQ, V) \
+    (slots == 8 ? go(route_backward_kernel<NQ, 8, V>) : slots == 16 ? go(route_backward_kernel<NQ, 16, V>) : go(route_backward_kernel<NQ, 32, V>))
+    if (p.N <= 128) return vec ? EXFOLD_BACK(1, true) : EXFOLD_BACK(1, false);
+    return vec ? EXFOLD_BACK(2, true) : EXFOLD_BACK(2, false);
+#undef EXFOLD_BACK
 }
 
 }  // namespace exfold
