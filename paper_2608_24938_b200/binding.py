@@ -82,6 +82,7 @@ class exfold_static_pool(C.Structure):
 
 
 class exfold_router(C.Structure):
+    bias_tensor = None  # make_router: what `bias` points to
     _fields_ = [("score", C.c_int32), ("n_groups", C.c_int32), ("top_groups", C.c_int32), ("group_score", C.c_int32),
                 ("renormalise", C.c_int32), ("scale", C.c_float), ("bias", C.c_void_p)]
 
@@ -424,6 +425,14 @@ def make_router(score: str = "softmax", bias: Optional[torch.Tensor] = None, n_g
     return r
 
 
+def _here(*tensors) -> None:
+    """The calls run on the current device: its tensors only (not the host's, nor another GPU's)."""
+    dev = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise AssertionError(f"tensor on {t.device}, the current device is cuda:{dev}")
+
+
 def _typed(t: Optional[torch.Tensor], dtype, shape) -> Optional[int]:
     if t is None:
         return None
@@ -435,9 +444,13 @@ def _typed(t: Optional[torch.Tensor], dtype, shape) -> Optional[int]:
 def exfold_route(layer, logits, router: exfold_router, ids, w, load=None, stream=None, check: bool = True) -> int:
     """logits [T][N] fp32 -> ids [T][K] int32, w [T][K] fp32, load [N] int32 (tokens per expert)."""
     T, N, K = logits.shape[0], layer.n_experts, layer.top_k
-    rc = lib.exfold_route(layer, _typed(logits, torch.float32, (T, N)), T, router, _typed(ids, torch.int32, (T, K)),
-                          _typed(w, torch.float32, (T, K)), _typed(load, torch.int32, (N,)) if load is not None else None,
-                          _stream(stream))
+    bias = router.bias_tensor
+    if bias is not None and bias.shape != (N,):
+        raise AssertionError(f"expected a bias of {N} experts, got {tuple(bias.shape)}")
+    args = (_typed(logits, torch.float32, (T, N)), T, router, _typed(ids, torch.int32, (T, K)), _typed(w, torch.float32, (T, K)),
+            _typed(load, torch.int32, (N,)))
+    _here(logits, bias, ids, w, load)
+    rc = lib.exfold_route(layer, *args, _stream(stream))
     if check and rc != 0:
         raise ExfoldError(rc, "exfold_route")
     return rc
@@ -446,9 +459,10 @@ def exfold_route(layer, logits, router: exfold_router, ids, w, load=None, stream
 def exfold_route_backward(layer, logits, ids, dw, router: exfold_router, dlogits, stream=None, check: bool = True) -> int:
     """dw [T][K], the gradient of exfold_route's weights -> dlogits [T][N]."""
     T, N, K = logits.shape[0], layer.n_experts, layer.top_k
-    rc = lib.exfold_route_backward(layer, _typed(logits, torch.float32, (T, N)), _typed(ids, torch.int32, (T, K)),
-                                   _typed(dw, torch.float32, (T, K)), T, router, _typed(dlogits, torch.float32, (T, N)),
-                                   _stream(stream))
+    args = (_typed(logits, torch.float32, (T, N)), _typed(ids, torch.int32, (T, K)), _typed(dw, torch.float32, (T, K)), T, router,
+            _typed(dlogits, torch.float32, (T, N)))
+    _here(logits, ids, dw, dlogits)
+    rc = lib.exfold_route_backward(layer, *args, _stream(stream))
     if check and rc != 0:
         raise ExfoldError(rc, "exfold_route_backward")
     return rc
@@ -460,6 +474,7 @@ def exfold_moe_prefill_routed(layer, x, ids, w, w_gate, w_up, w_down, tables: Op
     """exfold_moe_prefill_ex on given routes ids, w [T][K]. tables may be None where k_pre = K."""
     T, K = x.shape[0], layer.top_k
     opts = exfold_fold_opts(loss_threshold, int(rescale), int(confidence_split), int(gemm_path))
+    _here(x, ids, w, w_gate, w_up, w_down, y, ws)
     rc = lib.exfold_moe_prefill_routed(C.byref(layer), _ptr(x), _typed(ids, torch.int32, (T, K)),
                                        _typed(w, torch.float32, (T, K)), T, _ptr(w_gate), _ptr(w_up), _ptr(w_down),
                                        C.byref(tables) if tables is not None else None, k_pre, C.byref(opts), _ptr(y),
@@ -473,6 +488,7 @@ def exfold_moe_decode_routed(layer, x, ids, w, w_gate, w_up, w_down, tables: exf
                              meta: Optional[dict] = None, stream=None, check: bool = True) -> int:
     """exfold_moe_decode on given routes ids, w [B][K]."""
     B, K = x.shape[0], layer.top_k
+    _here(x, ids, w, w_gate, w_up, w_down, y, ws)
     rc = lib.exfold_moe_decode_routed(C.byref(layer), _ptr(x), _typed(ids, torch.int32, (B, K)),
                                       _typed(w, torch.float32, (B, K)), B, _ptr(w_gate), _ptr(w_up), _ptr(w_down),
                                       C.byref(tables), pool_m, _ptr(y), _decode_meta(meta), _ptr(ws), ws.numel(),
@@ -527,6 +543,7 @@ def exfold_linear(x, w, y, ws, bias=None, residual=None, activation: str = "none
         ldr = _rows(residual, out, T, o)
     if bias is not None and (bias.dtype is not dt or bias.shape != (o,) or not bias.is_contiguous()):
         raise AssertionError(f"expected bias {dt} {(o,)}, got {bias.dtype} {tuple(bias.shape)}")
+    _here(x, w, bias, residual, y, ws)
     rc = lib.exfold_linear(_linear_desc(i, o, _LINEAR_DTYPES[dt], _LINEAR_DTYPES[out], ACTIVATIONS[activation], ldx, ldw, ldy, ldr),
                            x.data_ptr(), w.data_ptr(), bias.data_ptr() if bias is not None else None,
                            residual.data_ptr() if residual is not None else None, T, y.data_ptr(), ws.data_ptr(), ws.numel(),

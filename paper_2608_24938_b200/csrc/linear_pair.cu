@@ -107,24 +107,25 @@ __device__ __forceinline__ void put_cols(unsigned char* buf, int lane, int h, co
     }
 }
 // The warp's 32 rows x 32 sums to memory, for y or a residual that no tensor map takes: through the buffer, so that a row's 32
-// columns are loaded and stored at once
+// columns are loaded and stored at once. add: the residual, lane = column, all rows asked for together and ahead (in batches of eight rows,
+// each behind the stores of the one before, 777 x 1411 x 2040 took 49 us)
 template <typename O>
-__device__ __forceinline__ void store_rows(const LinearParams& l, unsigned char* buf, int lane, const float (&f)[32], int64_t row0, int rows,
-                                           int col) {
+__device__ __forceinline__ void fetch_rows(const LinearParams& l, O (&add)[32], int64_t row0, int rows, int col) {
+    const O* r = reinterpret_cast<const O*>(l.residual) + row0 * l.ldr + col;
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+        if (i < rows && col < l.N) add[i] = r[i * l.ldr];
+}
+template <typename O>
+__device__ __forceinline__ void store_rows(const LinearParams& l, unsigned char* buf, int lane, const float (&f)[32], const O (&add)[32],
+                                           int64_t row0, int rows, int col) {
     put_cols<float>(buf, lane, 0, f, false);
     __syncwarp();
-    const bool in = col + lane < l.N;
     O* y = reinterpret_cast<O*>(l.y) + row0 * l.ldy + col + lane;
-    const O* r = reinterpret_cast<const O*>(l.residual) + row0 * l.ldr + col + lane;
-    for (int i0 = 0; i0 < rows; i0 += 8) {
-        float add[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) add[i] = l.residual != nullptr && in && i0 + i < rows ? linear_f32(r[(i0 + i) * l.ldr]) : 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float v = *reinterpret_cast<const float*>(buf + (i0 + i) * 128 + (((lane >> 2) ^ (i & 7)) << 4) + (lane & 3) * 4);
-            if (in && i0 + i < rows) linear_store(y + (i0 + i) * l.ldy, l.residual != nullptr ? v + add[i] : v);
-        }
+    for (int i = 0; i < 32; ++i) {
+        const float v = *reinterpret_cast<const float*>(buf + i * 128 + (((lane >> 2) ^ (i & 7)) << 4) + (lane & 3) * 4);
+        if (i < rows && col + lane < l.N) linear_store(y + i * l.ldy, l.residual != nullptr ? v + linear_f32(add[i]) : v);
     }
     __syncwarp();
 }
@@ -278,6 +279,9 @@ __global__ void __launch_bounds__(kLpThreads, 1) linear_pair_kernel(const __grid
                 ptx::mbar_expect_tx(rbar, kLpOutBytes);
                 ptx::tma_load_2d(buf, &p.tm_r, rbar, col0, (int)row0);
             }
+            O add[TMA ? 1 : 32];
+            if constexpr (!TMA)
+                if (some && has_res) fetch_rows<O>(p.l, add, row0, rows, col0 + lane);
             if (lane == 0) ok = ptx::mbar_wait_local(&tfull_bar[as], aphase, abort_flag, p.l.status, 4) ? 1 : 0;
             ok = __shfl_sync(0xffffffffu, ok, 0);
             if (!ok) break;
@@ -318,16 +322,20 @@ __global__ void __launch_bounds__(kLpThreads, 1) linear_pair_kernel(const __grid
                     }
                 }
                 if (!ok) break;
-            } else if (!TMA && some) {
+            }
+            if constexpr (!TMA) {
+                if (some) {
 #pragma unroll 1
-                for (int col = col0; col < min(col0 + 128, p.l.N); col += 32) {
-                    uint32_t v[32];
-                    float f[32];
-                    ptx::tmem_ld32(taddr + col - col0, v);
-                    ptx::tmem_ld_wait();
-                    if (full_bias && col + 32 <= p.l.N) bias_act<true>(f, v, p.l, col);
-                    else bias_act<false>(f, v, p.l, col);
-                    store_rows<O>(p.l, buf, lane, f, row0, rows, col);
+                    for (int col = col0; col < min(col0 + 128, p.l.N); col += 32) {
+                        uint32_t v[32];
+                        float f[32];
+                        ptx::tmem_ld32(taddr + col - col0, v);
+                        ptx::tmem_ld_wait();
+                        if (full_bias && col + 32 <= p.l.N) bias_act<true>(f, v, p.l, col);
+                        else bias_act<false>(f, v, p.l, col);
+                        store_rows<O>(p.l, buf, lane, f, add, row0, rows, col);
+                        if (has_res && col + 32 < col0 + 128) fetch_rows<O>(p.l, add, row0, rows, col + 32 + lane);
+                    }
                 }
             }
             ptx::tc_fence_before();

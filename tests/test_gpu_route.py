@@ -233,6 +233,21 @@ def test_route_captured_and_on_another_stream(ex):
         assert torch.equal(eager, dz)
 
 
+def test_route_refuses_tensors_of_the_host(ex):
+    layer, r = ex.make_layer(8, 0, 64, 64, 2, "f32"), ex.make_router()
+    z, ids, w = torch.zeros(3, 8, device="cuda"), torch.zeros(3, 2, dtype=torch.int32, device="cuda"), torch.zeros(3, 2, device="cuda")
+    for bad in ((z.cpu(), ids, w), (z, ids.cpu(), w), (z, ids, w.cpu())):
+        with pytest.raises(AssertionError):
+            ex.exfold_route(layer, bad[0], r, bad[1], bad[2])
+    with pytest.raises(AssertionError):
+        ex.exfold_route_backward(layer, z, ids, w, r, z.cpu())
+    x = torch.zeros(2, 64, dtype=torch.bfloat16, device="cuda")
+    ws = ex.alloc_linear_workspace(64, 2, 2, torch.bfloat16)
+    for bad in ((x.cpu(), x, ws), (x, x.cpu(), ws), (x, x, ws.cpu())):
+        with pytest.raises(AssertionError):
+            ex.exfold_linear(bad[0], bad[1], torch.zeros(2, 2, dtype=torch.bfloat16, device="cuda"), bad[2])
+
+
 # ------------------------------------------------------------------------------------------------ gradient
 def grad64(z, ids, g, score, renormalise, scale):
     s, _ = scores64(z.astype(np.float64), score)
@@ -264,7 +279,8 @@ def grad_bound(z, ids, g, score, renormalise, scale):
     dot = (a * s[rows, ids]).sum(1, keepdims=True)
     terms = s * dot
     np.add.at(terms, (np.broadcast_to(rows, ids.shape), ids), a * s[rows, ids])
-    spread = np.where(masked, 0.0, z.max(1, keepdims=True) - z).max()
+    with np.errstate(invalid="ignore"):
+        spread = np.where(masked, 0.0, z.max(1, keepdims=True) - z).max()
     return 2 * (spread + 4 + 13 + 2 + 7) * 2.0 ** -24 * terms + 2.0 ** -126
 
 

@@ -104,5 +104,9 @@ def test_binding_refuses_what_the_call_cannot_see(ex):
         ex.exfold_route(layer, torch.zeros(4, 8), ex.make_router(), torch.zeros(4, 2, dtype=torch.int64), torch.zeros(4, 2))
     with pytest.raises(AssertionError):
         ex.exfold_route(layer, torch.zeros(4, 9), ex.make_router(), torch.zeros(4, 2, dtype=torch.int32), torch.zeros(4, 2))
+    with pytest.raises(AssertionError):  # a bias of another layer
+        ex.exfold_route(layer, torch.zeros(4, 8), ex.make_router(bias=torch.zeros(7)), torch.zeros(4, 2, dtype=torch.int32), torch.zeros(4, 2))
+    with pytest.raises(AssertionError):
+        ex.make_router(bias=torch.zeros(8, dtype=torch.float64))
     with pytest.raises(KeyError):
         ex.make_router("tanh")
