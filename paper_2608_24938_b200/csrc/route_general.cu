@@ -17,9 +17,9 @@
 // s (1 - s) times: below 1.3; the sum 1, the quotient 4. Softmax: the argument's rounding counts d e^-d <= 0.4, expf 4, the sum 13, the
 // quotient 4: below 22. And the addition's half step of the choice. Two choices are sure of their order if further apart than twice that.
 //
-// GPU time, 64-bit choices for every token -> now (sigmoid, bias, Top-8): 16384 tokens x 128 experts 23.2 -> 12.7 us, 777 x 256 in 8 groups
+// GPU time, 64-bit choices for every token -> now (sigmoid, bias, Top-8): 16384 tokens x 128 experts 23.2 -> 10.6 us, 777 x 256 in 8 groups
 // with the load 13.2 -> 6.3, one token 4.4 -> 2.5; gradient, a token per warp -> now: 16384 x 128 13.0 -> 3.8, softmax over all experts 6.9.
-// Ranking by one word (24 bits of the choice, 8 of the expert: one reduction per round instead of two) took 12.1 and 6.9 us.
+// Ranking by one word (24 bits of the choice, 8 of the expert: one reduction per round instead of two) took 12.1 and 6.9 us (blocks of 256 threads: 12.8 and 5.9).
 #include <algorithm>
 
 #include "common.cuh"
@@ -218,9 +218,13 @@ __global__ void __launch_bounds__(kMaxExperts) clear_load_kernel(int32_t* load, 
     if ((int)threadIdx.x < N) load[threadIdx.x] = 0;
 }
 
+// Blocks of 128 threads up to 128 experts: the compiler may use more registers, and an SM gets the next warps sooner (16384 tokens of 128
+// experts 12.8 -> 10.6 us; 777 tokens of 256 experts in groups 5.9 -> 7.3)
+constexpr int route_threads(int npl) { return npl <= 4 ? 128 : kGrThreads; }
+
 // SLOTS: lanes per token when the weights are computed, K rounded up to 8, 16 or 32; a warp takes `batch` <= 32 / SLOTS tokens at a time
 template <int NPL, int SLOTS>
-__global__ void __launch_bounds__(kGrThreads) route_general_kernel(const __grid_constant__ RouteGeneralParams p) {
+__global__ void __launch_bounds__(route_threads(NPL)) route_general_kernel(const __grid_constant__ RouteGeneralParams p) {
     extern __shared__ unsigned long long s_key[];  // [warps][N]
     __shared__ int hist[kMaxExperts];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = (int)blockDim.x >> 5;
@@ -496,11 +500,11 @@ __global__ void __launch_bounds__(kGrThreads) route_backward_kernel(const __grid
 }  // namespace
 
 cudaError_t launch_route_general(RouteGeneralParams p, int sms, cudaStream_t s) {
-    constexpr int kWarps = kGrThreads / 32;
+    const int threads = route_threads((p.N + 31) / 32), kWarps = threads / 32;
     const int slots = p.K <= 8 ? 8 : p.K <= 16 ? 16 : 32;
     // Long prompts: several tokens of a warp share the 64-bit part; short ones take a warp each, it is one token's chain of latencies then
-    p.batch = p.T >= (int64_t)sms * kWarps * 4 ? 32 / slots : 1;
-    const unsigned blocks = (unsigned)std::max<int64_t>(1, std::min<int64_t>((p.T + kWarps * p.batch - 1) / (kWarps * p.batch), (int64_t)8 * sms));
+    p.batch = p.T >= (int64_t)sms * 32 ? 32 / slots : 1;
+    const unsigned blocks = (unsigned)std::max<int64_t>(1, std::min<int64_t>((p.T + kWarps * p.batch - 1) / (kWarps * p.batch), (int64_t)8 * sms * (kGrThreads / threads)));
     // load: several CTAs add theirs up in memory, which a kernel clears first (a memset, which the next kernel cannot be launched under,
     // took 3.5 us of a call; CTAs of a cluster that add up between themselves, for 64 tokens, 0.9 us more than this)
     if (p.load != nullptr && (blocks > 1 || p.T == 0)) {
@@ -509,7 +513,7 @@ cudaError_t launch_route_general(RouteGeneralParams p, int sms, cudaStream_t s) 
     }
     if (p.T == 0) return cudaSuccess;
     const size_t smem = p.n_groups > 1 ? (size_t)kWarps * p.N * sizeof(unsigned long long) : 0;
-    auto go = [&](auto kernel) { return launch_pdl(kernel, blocks, kGrThreads, smem, s, p); };
+    auto go = [&](auto kernel) { return launch_pdl(kernel, blocks, threads, smem, s, p); };
 #define EXFOLD_ROUTE(NPL) \
     return slots == 8 ? go(route_general_kernel<NPL, 8>) : slots == 16 ? go(route_general_kernel<NPL, 16>) : go(route_general_kernel<NPL, 32>)
     switch ((p.N + 31) / 32) {
