@@ -1290,7 +1290,7 @@ int exfold_linear(const exfold_linear_desc* desc, const void* x, const void* w, 
         p.K = (int)packed_row(desc); p.ldx = p.ldw = p.K;
     }
     if (bf16 && aligned16(x) && aligned16(w) && ((p.ldx | p.ldw) & 7) == 0) {
-        if (linear_small_fits(p)) {
+        if (linear_small_fits(p, sm_count())) {
             EXFOLD_CUDA(launch_linear_small(p, out_bf16, sm_count(), s));
         } else if (linear_prefers_pairs(T, p.N, p.K, sm_count())) {
             LinearPairParams q{};

@@ -488,7 +488,7 @@ cudaError_t launch_linear_simt(const LinearParams& p, bool bf16, bool out_bf16, 
 // Copies of x and w (bf16) with rows of `to` elements, zeros behind K (linear.cu)
 cudaError_t launch_linear_pack(const LinearParams& p, void* xp, void* wp, int to, int sms, cudaStream_t s);
 // bf16, at most 8 tokens (linear_small.cu)
-bool linear_small_fits(const LinearParams& p);
+bool linear_small_fits(const LinearParams& p, int sms);
 cudaError_t launch_linear_small(const LinearParams& p, bool out_bf16, int sms, cudaStream_t s);
 // bf16 on the tensor cores, K split over a cluster (linear_tile.cu)
 struct LinearTilePlan {

@@ -161,8 +161,12 @@ __global__ void __launch_bounds__(32 * kSmMaxWarps, 1) linear_small_kernel(Linea
 
 }  // namespace
 
-// Whether this kernel takes a call (both operands start on 16-byte boundaries, with rows multiples of 8 elements apart)
-bool linear_small_fits(const LinearParams& p) { return p.T <= 8 && p.K % 8 == 0; }
+// Whether this kernel takes a call (both operands start on 16-byte boundaries, with rows multiples of 8 elements apart). Up to two rounds
+// of items: every round starts with empty pipes. This kernel / linear_tile.cu, on the GPU with bias and residual (tokens x features x K):
+// 1 x 4096 x 4096 8.9 / 9.7 us, 1 x 768 x 2048 3.8 / 4.3, 4 x 6144 x 4096 14.2 / 18.3, 1 x 8192 x 2048 9.5 / 9.8, 1 x 14336 x 4096 24.9 / 21.1,
+// 8 x 14336 x 1024 13.2 / 9.0. (A persistent form, the next item's weights asked for while one item's sums meet, spilled registers:
+// 1 x 4096 x 4096 9.4 us, 1 x 14336 x 4096 25.3.)
+bool linear_small_fits(const LinearParams& p, int sms) { return p.T <= 8 && p.K % 8 == 0 && (p.N + 15) / 16 <= 4 * sms; }
 
 cudaError_t launch_linear_small(const LinearParams& p, bool out_bf16, int sms, cudaStream_t s) {
     const bool wide = ((reinterpret_cast<uintptr_t>(p.x) | reinterpret_cast<uintptr_t>(p.w)) & 31) == 0 && ((p.ldx | p.ldw | p.K) & 15) == 0;
