@@ -362,8 +362,12 @@ __global__ void __launch_bounds__(kLpThreads, 1) linear_pair_kernel(const __grid
 cudaError_t launch_linear_pair(LinearPairParams p, bool out_bf16, int sms, cudaStream_t s) {
     p.mt = (int)((p.l.T + 255) / 256);
     p.nt = (p.l.N + 255) / 256;
-    // The row tiles of a band stay in L2 while the weights pass by
-    p.band = (int)std::max<int64_t>(1, std::min<int64_t>(p.mt, (48 << 20) / ((int64_t)p.l.K * 512)));
+    // Bands of 16 MB of token rows, which stay in L2 while the weights pass by (and the pairs that run together share few of both). In
+    // long loops, at the power limit, 8 / 16 / 32 / 48 / 64 MB and one band: 8192 x 4096 x 4096 202 / 215 / 213 / 220 / 231 / 238 us, 16384 x
+    // 4096 x 4096 437 / 430 / 434 / 455 / 506 / 554, 8192 x 14336 x 4096 802 / 749 / 760 / 797 / 849 / 846.
+    p.band = (int)std::max<int64_t>(1, std::min<int64_t>(p.mt, (16 << 20) / ((int64_t)p.l.K * 512)));
+    const int bands = (p.mt + p.band - 1) / p.band;
+    p.band = (p.mt + bands - 1) / bands;
     if ((int64_t)p.mt * p.nt > 0x3fffffff) return cudaErrorInvalidValue;
     const int total = p.mt * p.nt, pairs = std::max(1, sms / 2), rounds = (total + pairs - 1) / pairs;
     const int grid = 2 * ((total + rounds - 1) / rounds);  // the pairs that take work finish together
