@@ -313,13 +313,13 @@ typedef struct {
     int32_t group_score; /* EXFOLD_GROUP_* */
     int32_t renormalise; /* != 0: the chosen scores are divided by their sum */
     float scale;         /* finite */
-    const float *bias;   /* [N] (device) or NULL */
+    const float *bias;   /* [N] (device, finite) or NULL */
 } exfold_router;
 
 /*
  * logits [T][N] fp32 -> ids [T][K] int32, w [T][K] fp32 and, if not NULL, load [N] int32: how many tokens chose each
  * expert (overwritten). `layer` gives N and K. T in [0, 2^24] (T = 0: load is cleared). No workspace; one kernel, with a
- * load and more than 8 tokens a kernel before it that clears it. Counts are added up with integer atomics: the same inputs give
+ * load and more than a few tokens a kernel before it that clears it. Counts are added up with integer atomics: the same inputs give
  * the same bits. ids and w are the arguments of exfold_moe_prefill_routed / exfold_moe_decode_routed.
  */
 int exfold_route(const exfold_layer *layer, const float *logits, int64_t T, const exfold_router *router, int32_t *ids,

@@ -210,3 +210,40 @@ def test_linear_is_reproducible_and_captured(ex, T):
         ex.exfold_linear(x, w, y, ws, stream=a)
     torch.cuda.synchronize()
     assert torch.equal(y, ref * 2)
+
+
+@pytest.mark.parametrize("dtype,out", [(torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32), (torch.float32, torch.float32)])
+@pytest.mark.parametrize("T", [3, 9])
+def test_linear_rows_far_apart(ex, dtype, out, T):
+    """Row offsets beyond 2^31 elements, of x and of y (in place on the residual)."""
+    i, o, ld = 128, 64, ((1 << 31) // (T - 1) + 64) // 8 * 8
+    x = torch.empty((T - 1) * ld + i, dtype=dtype, device="cuda").as_strided((T, i), (ld, 1))
+    y = torch.empty((T - 1) * ld + o, dtype=out, device="cuda").as_strided((T, o), (ld, 1))
+    g = torch.Generator(device="cuda").manual_seed(3)
+    w = (torch.randn((o, i), generator=g, device="cuda") * i ** -0.5).to(dtype)
+    x.copy_(torch.randn((T, i), generator=g, device="cuda").to(dtype))
+    y.copy_(torch.randn((T, o), generator=g, device="cuda").to(out))
+    ref, bound = reference(x, w, None, y, "silu", out)
+    ws = ex.alloc_linear_workspace(i, o, T, dtype, out, ldx=ld)
+    ex.exfold_linear(x, w, y, ws, residual=y, activation="silu")
+    assert ex.exfold_device_status(ws) == 0
+    assert ((y.double() - ref).abs() <= bound).all()
+
+
+def test_linear_one_workspace_on_one_stream(ex):
+    """Calls of different sizes and types one after the other on a stream share a workspace as large as the largest needs."""
+    sizes = [(1, 65, 64), (300, 333, 129), (8, 64, 64), (64, 517, 200), (700, 256, 512), (3, 1411, 8)]
+    need = max(ex.alloc_linear_workspace(i, o, t, torch.bfloat16).numel() for t, i, o in sizes)
+    ws = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+    calls = []
+    for n, (t, i, o) in enumerate(sizes * 2):
+        g = torch.Generator(device="cuda").manual_seed(n)
+        x = torch.randn((t, i), generator=g, device="cuda").bfloat16()
+        w = (torch.randn((o, i), generator=g, device="cuda") * i ** -0.5).bfloat16()
+        calls.append((x, w, torch.empty((t, o), dtype=torch.bfloat16, device="cuda")))
+    for x, w, y in calls:
+        ex.exfold_linear(x, w, y, ws, activation="relu")
+    assert ex.exfold_device_status(ws) == 0
+    for x, w, y in calls:
+        ref, bound = reference(x, w, None, None, "relu", torch.bfloat16)
+        assert ((y.double() - ref).abs() <= bound).all()

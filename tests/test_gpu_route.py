@@ -353,3 +353,27 @@ def test_route_backward_against_differences(ex, score, renormalise):
     got = run_back(ex, z, ids, g, score, renormalise, 2.0)
     tol = 2 * 2.0 * np.abs(g).sum(1).max() * 1e-8 / 6 + 1e-8 + grad_bound(z, ids, g, score, renormalise, 2.0)
     assert bool((np.abs(got - num) <= tol).all())
+
+
+def test_route_beyond_32_bit_offsets(ex):
+    """More than 2^31 scores: the last tokens' rows are found, and nothing else is written there."""
+    N, K, T = 256, 2, (1 << 23) + 5
+    z = torch.zeros((T, N), device="cuda")
+    tail = scores(5, N, seed=31)
+    z[-5:] = torch.from_numpy(tail).cuda()
+    layer, r = ex.make_layer(N, 0, 64, 64, K, "f32"), ex.make_router("softmax")
+    ids, w = torch.empty((T, K), dtype=torch.int32, device="cuda"), torch.empty((T, K), device="cuda")
+    load = torch.empty(N, dtype=torch.int32, device="cuda")
+    ex.exfold_route(layer, z, r, ids, w, load)
+    rid, rw = route64(tail, K, "softmax")
+    assert np.array_equal(ids[-5:].cpu().numpy(), rid) and torch.equal(ids[:-5].amax(0).cpu(), torch.tensor([0, 1], dtype=torch.int32))
+    assert bool((np.abs(w[-5:].cpu().numpy() - rw) <= rw * (2.0 ** -24 + 1e-12)).all())
+    assert int(load.sum()) == T * K and int(load[0]) >= T - 5
+    dz = torch.full((T, N), float("nan"), device="cuda")
+    g = torch.ones((T, K), device="cuda")
+    g[:, 1] = -1.0
+    ex.exfold_route_backward(layer, z, ids, g, r, dz)
+    ref = grad64(tail, rid, g[-5:].cpu().numpy(), "softmax", True, 1.0)
+    bound = grad_bound(tail, rid, g[-5:].cpu().numpy(), "softmax", True, 1.0)
+    assert bool((np.abs(dz[-5:].cpu().numpy() - ref) <= bound).all())
+    assert torch.equal(dz[:-5].amax(0)[:2].cpu(), torch.tensor([0.5, -0.5])) and torch.equal(dz[:-5, 2:].abs().amax(), dz.new_zeros(()))
