@@ -366,7 +366,7 @@ int exfold_moe_decode_routed(const exfold_layer *layer, const void *x, const int
  * and ldw multiples of 8 elements and x and w 16-byte aligned the operands are read in place; where a distance is no multiple
  * of 8, x and w are first copied to aligned rows in the workspace; operands that only start unaligned, and fp32 ones, run on
  * a CUDA-core kernel.
- * Results do not depend on other calls: no atomics, sums in a fixed order for the given sizes.
+ * Results do not depend on other calls: no atomics, sums in a fixed order for the given sizes, distances and alignment.
  * Workspace: exfold_linear_workspace_bytes of the same description (256-byte aligned; its first 256 bytes are the status
  * record of exfold_device_status). Calls that share a workspace must be ordered on one stream.
  */

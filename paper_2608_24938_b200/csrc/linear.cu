@@ -6,9 +6,9 @@
 //       are reduced over the lanes by halving exchanges (62 shuffles) and meet in shared memory, in order.
 //   tiles        64 x 64 outputs per CTA of 128 threads, 8 x 4 of them per thread; K in steps of 16 through two shared-memory stages,
 //       the next step's loads in registers meanwhile. Rows lie along K with a pitch of 20 floats: what a quarter warp reads in 16-byte
-//       pieces hits distinct banks. Bound by those reads (shared memory returns 128 bytes per cycle; 8 x 4 outputs need 48 bytes per
-//       thread for 32 multiply-adds) and by latency: K is split over a cluster (LinearReduce) until four CTAs share an SM. 128 x 64
-//       tiles with 8 x 8 outputs per thread need 254 registers and were slower at every size: 512 x 2048 x 1024 75 us against 69.
+//       pieces hits distinct banks. K is split over a cluster (LinearReduce) until four CTAs share an SM.
+//   large tiles  128 x 128 outputs per CTA of 256 threads, 8 x 8 per thread, stages transposed, two multiply-adds per instruction
+//       (fma.rn.f32x2; with single ones both kernels stop at 32 TFLOP/s, half of what the packed form can do).
 #include <algorithm>
 
 #include "common.cuh"
@@ -28,6 +28,13 @@ __device__ __forceinline__ float4 load4(const T* p, int left) {
     if (left > 2) v.z = linear_f32(p[2]);
     if (left > 3) v.w = linear_f32(p[3]);
     return v;
+}
+
+// c += a b, both halves: one instruction
+__device__ __forceinline__ void fma2(float2& c, const float2& a, const float2& b) {
+    asm("fma.rn.f32x2 %0, %1, %2, %0;"
+        : "+l"(reinterpret_cast<unsigned long long&>(c))
+        : "l"(reinterpret_cast<const unsigned long long&>(a)), "l"(reinterpret_cast<const unsigned long long&>(b)));
 }
 
 // ---------------------------------------------------------------- few tokens
@@ -202,6 +209,97 @@ __global__ void __launch_bounds__(kLsThreads) linear_simt_kernel(LinearParams p)
     if (SPLIT > 1) cooperative_groups::this_cluster().sync();  // no CTA leaves while its part may still be read
 }
 
+// ---------------------------------------------------------------- large tiles
+// 128 x 128 outputs per CTA of 256 threads, 8 x 8 of them per thread. Stages lie transposed (a k's rows next to each other), so that a
+// thread reads the 16 operands of a k in four 16-byte pieces and holds no more of them than that: 64 bytes for 64 multiply-adds, the rate at
+// which shared memory returns them.
+constexpr int kLbThreads = 256, kLbTile = 128, kLbPitch = kLbTile + 4;
+
+template <typename T, typename O, bool VEC, int SPLIT>
+__global__ void __launch_bounds__(kLbThreads, 1) linear_simt_big_kernel(LinearParams p) {
+    constexpr int kPart = kLbTile + 1, kStage = 2 * kLsBK * kLbPitch;
+    extern __shared__ __align__(16) float smem[];  // two stages of both operands; then the partial tile
+    const T* x = reinterpret_cast<const T*>(p.x);
+    const T* w = reinterpret_cast<const T*>(p.w);
+    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+    const int n_tiles = (p.N + kLbTile - 1) / kLbTile;
+    const int rank = (int)blockIdx.x % SPLIT, tile = (int)blockIdx.x / SPLIT;
+    const int64_t m0 = (int64_t)(tile / n_tiles) * kLbTile;
+    const int n0 = tile % n_tiles * kLbTile;
+    const int steps = (p.K + kLsBK - 1) / kLsBK, s0 = (int)((int64_t)rank * steps / SPLIT), s1 = (int)((int64_t)(rank + 1) * steps / SPLIT);
+    grid_dep_launch();
+    grid_dep_wait();
+    if (blockIdx.x == 0 && tid < 4) reinterpret_cast<int*>(p.status)[tid] = 0;
+    // thread t loads rows t / 4 and t / 4 + 64 of both operands, four elements at 4 (t % 4)
+    const int lrow = tid >> 2, lk = (tid & 3) * 4;
+    const T* px[2];
+    const T* pw[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        px[u] = x + min(m0 + lrow + 64 * u, p.T - 1) * p.ldx + lk;
+        pw[u] = w + (int64_t)min(n0 + lrow + 64 * u, p.N - 1) * p.ldw + lk;
+    }
+    float4 ra[2], rb[2];
+    auto load = [&](int s) {
+        const int left = p.K - s * kLsBK - lk;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            ra[u] = load4<VEC>(px[u] + (int64_t)s * kLsBK, left);
+            rb[u] = load4<VEC>(pw[u] + (int64_t)s * kLsBK, left);
+        }
+    };
+    auto store = [&](int buf) {
+        float* a = smem + buf * kStage + lk * kLbPitch + lrow;
+        float* b = a + kLsBK * kLbPitch;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            a[64 * u] = ra[u].x; a[kLbPitch + 64 * u] = ra[u].y; a[2 * kLbPitch + 64 * u] = ra[u].z; a[3 * kLbPitch + 64 * u] = ra[u].w;
+            b[64 * u] = rb[u].x; b[kLbPitch + 64 * u] = rb[u].y; b[2 * kLbPitch + 64 * u] = rb[u].z; b[3 * kLbPitch + 64 * u] = rb[u].w;
+        }
+    };
+    // outputs of this thread: rows 4 ty + i and 64 + 4 ty + i, columns 4 tx + j and 64 + 4 tx + j
+    float2 acc[8][4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = make_float2(0.f, 0.f);
+    load(s0);
+    store(0);
+    __syncthreads();
+    int buf = 0;
+    for (int s = s0; s < s1; ++s, buf ^= 1) {
+        if (s + 1 < s1) load(s + 1);
+        const float* sa = smem + buf * kStage + 4 * ty;
+        const float* sb = smem + buf * kStage + kLsBK * kLbPitch + 4 * tx;
+#pragma unroll 4
+        for (int k = 0; k < kLsBK; ++k) {
+            const float4 a0 = *reinterpret_cast<const float4*>(sa + k * kLbPitch), a1 = *reinterpret_cast<const float4*>(sa + k * kLbPitch + 64);
+            const float4 b0 = *reinterpret_cast<const float4*>(sb + k * kLbPitch), b1 = *reinterpret_cast<const float4*>(sb + k * kLbPitch + 64);
+            const float a[8] = {a0.x, a0.y, a0.z, a0.w, a1.x, a1.y, a1.z, a1.w};
+            const float2 b[4] = {make_float2(b0.x, b0.y), make_float2(b0.z, b0.w), make_float2(b1.x, b1.y), make_float2(b1.z, b1.w)};
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) fma2(acc[i][j], make_float2(a[i], a[i]), b[j]);
+        }
+        if (s + 1 < s1) store(buf ^ 1);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            smem[((i >> 2) * 64 + 4 * ty + (i & 3)) * kPart + (j >> 2) * 64 + 4 * tx + (j & 3)] = (j & 1) ? acc[i][j >> 1].y : acc[i][j >> 1].x;
+    const LinearEpilogue<O> ep(p);
+    LinearReduce<SPLIT, O, kLbThreads, false, T> reduce(ep, (int)min((int64_t)kLbTile, p.T - m0), kLbTile, m0, n0, rank, tid);
+    reduce.begin();
+    if (SPLIT > 1) cooperative_groups::this_cluster().sync();
+    else __syncthreads();
+    reduce.run(smem, kPart, 0, 1);
+    if (SPLIT > 1) cooperative_groups::this_cluster().sync();  // no CTA leaves while its part may still be read
+}
+constexpr size_t kLbSmem = sizeof(float) * (2 * 2 * kLsBK * kLbPitch > kLbTile * (kLbTile + 1) ? 2 * 2 * kLsBK * kLbPitch : kLbTile * (kLbTile + 1));
+
 template <typename T, typename O, bool VEC>
 cudaError_t launch_simt_t(const LinearParams& p, int sms, cudaStream_t s) {
     // few tokens / tiles: 32 x 1024 x 1024 11.1 / 15.2 us, 32 x 2000 x 2000 31.4 / 32.1, 48 x 512 x 512 5.2 / 6.2, 64 x 256 x 128 3.0 / 4.1,
@@ -212,6 +310,26 @@ cudaError_t launch_simt_t(const LinearParams& p, int sms, cudaStream_t s) {
     }
     const int64_t tiles = ((p.T + kLsBM - 1) / kLsBM) * ((p.N + kLsBN - 1) / kLsBN);
     if (tiles > 0x0fffffff) return cudaErrorInvalidValue;
+    // Large tiles: a CTA per SM at 0.31 TFLOP/s, 1.7 us per step of 16 and 5 us for itself, with the split that fills the SMs best; the small
+    // ones, 32 TFLOP/s together. Small / large: 1024 x 2000 x 1000 (tokens x features x K) 137 / 109 us, 1024 x 1000 x 2048 131 / 114, 512 x 2048 x 1024 69 / 62, 256 x
+    // 2048 x 2048 68 / 60, 1000 x 500 x 500 22 / 23, 300 x 700 x 1000 21.6 / 34.
+    const int64_t big = ((p.T + kLbTile - 1) / kLbTile) * ((p.N + kLbTile - 1) / kLbTile), steps = (p.K + kLsBK - 1) / kLsBK;
+    int big_split = 1;
+    auto us = [&](int q) { return (double)((big * q + sms - 1) / sms) * (1.7 * (double)((steps + q - 1) / q) + 5.0); };
+    for (int q = 2; q <= 8 && q * 2 <= steps; q *= 2)
+        if (us(q) < us(big_split)) big_split = q;
+    if (us(big_split) < 2.0 * (double)p.T * p.N * p.K / 32e6 + 5.0) {
+        auto go = [&](auto kernel) {
+            const cudaError_t e = ensure_smem(kernel, kLbSmem);
+            return e != cudaSuccess ? e : launch_pdl_cluster(kernel, (unsigned)(big * big_split), kLbThreads, kLbSmem, big_split, s, p);
+        };
+        switch (big_split) {
+            case 1: return go(linear_simt_big_kernel<T, O, VEC, 1>);
+            case 2: return go(linear_simt_big_kernel<T, O, VEC, 2>);
+            case 4: return go(linear_simt_big_kernel<T, O, VEC, 4>);
+            default: return go(linear_simt_big_kernel<T, O, VEC, 8>);
+        }
+    }
     // 64 x 1024 x 1024 (tokens x features x K) in 1 / 2 / 4 / 8 parts 63.0 / 29.5 / 17.3 / 16.0 us, 300 x 700 x 1000 62.9 / 46.4 / 35.1 /
     // 21.6, 1000 x 500 x 500 57.7 / 37.0 / 22.2 / 27.1, 1024 x 1000 x 2048 259 / 131 / 133 / 130
     int split = 1;
