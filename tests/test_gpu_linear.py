@@ -247,3 +247,27 @@ def test_linear_one_workspace_on_one_stream(ex):
     for x, w, y in calls:
         ref, bound = reference(x, w, None, None, "relu", torch.bfloat16)
         assert ((y.double() - ref).abs() <= bound).all()
+
+
+def test_linear_kernels_beside_each_other(ex):
+    """Calls of every kernel on streams of their own, at the same time: each has the bits it has alone."""
+    sizes = [(1, 1024, 2048, torch.bfloat16), (40, 2048, 1024, torch.bfloat16), (300, 1024, 1024, torch.bfloat16), (100, 2048, 40, torch.bfloat16),
+             (2500, 1024, 2048, torch.bfloat16), (70, 517, 333, torch.bfloat16), (100, 512, 512, torch.float32), (6, 512, 512, torch.float32)]
+    jobs = []
+    for n, (t, i, o, dtype) in enumerate(sizes):
+        g = torch.Generator(device="cuda").manual_seed(n)
+        x = torch.randn((t, i), generator=g, device="cuda").to(dtype)
+        w = (torch.randn((o, i), generator=g, device="cuda") * i ** -0.5).to(dtype)
+        r = torch.randn((t, o), generator=g, device="cuda").to(dtype)
+        alone, y = torch.empty_like(r), torch.empty_like(r)
+        ws = ex.alloc_linear_workspace(i, o, t, dtype)
+        ex.exfold_linear(x, w, alone, ws, residual=r, activation="silu")
+        assert ex.exfold_device_status(ws) == 0
+        jobs.append((x, w, y, ws, r, alone, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(30):
+        for x, w, y, ws, r, _, stream in jobs:
+            ex.exfold_linear(x, w, y, ws, residual=r, activation="silu", stream=stream)
+    torch.cuda.synchronize()
+    for x, w, y, ws, r, alone, _ in jobs:
+        assert ex.exfold_device_status(ws) == 0 and torch.equal(y, alone)
