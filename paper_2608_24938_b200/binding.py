@@ -443,14 +443,19 @@ def _typed(t: Optional[torch.Tensor], dtype, shape) -> Optional[int]:
 
 def exfold_route(layer, logits, router: exfold_router, ids, w, load=None, stream=None, check: bool = True) -> int:
     """logits [T][N] fp32 -> ids [T][K] int32, w [T][K] fp32, load [N] int32 (tokens per expert)."""
-    T, N, K = logits.shape[0], layer.n_experts, layer.top_k
-    bias = router.bias_tensor
+    (T, N), K, bias = logits.shape, layer.top_k, router.bias_tensor
+    if not (logits.dtype is torch.float32 and N == layer.n_experts and ids.dtype is torch.int32 and w.dtype is torch.float32 and
+            ids.shape == w.shape == (T, K) and logits.is_contiguous() and ids.is_contiguous() and w.is_contiguous()):
+        _typed(logits, torch.float32, (T, layer.n_experts)), _typed(ids, torch.int32, (T, K)), _typed(w, torch.float32, (T, K))
     if bias is not None and bias.shape != (N,):
         raise AssertionError(f"expected a bias of {N} experts, got {tuple(bias.shape)}")
-    args = (_typed(logits, torch.float32, (T, N)), T, router, _typed(ids, torch.int32, (T, K)), _typed(w, torch.float32, (T, K)),
-            _typed(load, torch.int32, (N,)))
-    _here(logits, bias, ids, w, load)
-    rc = lib.exfold_route(layer, *args, _stream(stream))
+    load_ptr = _typed(load, torch.int32, (N,)) if load is not None else None
+    dev = torch._C._cuda_getDevice()
+    if not (logits.get_device() == ids.get_device() == w.get_device() == dev and (bias is None or bias.get_device() == dev) and
+            (load is None or load.get_device() == dev)):
+        _here(logits, bias, ids, w, load)
+    rc = lib.exfold_route(layer, logits.data_ptr(), T, router, ids.data_ptr(), w.data_ptr(), load_ptr,
+                          stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(dev))
     if check and rc != 0:
         raise ExfoldError(rc, "exfold_route")
     return rc
@@ -458,11 +463,17 @@ def exfold_route(layer, logits, router: exfold_router, ids, w, load=None, stream
 
 def exfold_route_backward(layer, logits, ids, dw, router: exfold_router, dlogits, stream=None, check: bool = True) -> int:
     """dw [T][K], the gradient of exfold_route's weights -> dlogits [T][N]."""
-    T, N, K = logits.shape[0], layer.n_experts, layer.top_k
-    args = (_typed(logits, torch.float32, (T, N)), _typed(ids, torch.int32, (T, K)), _typed(dw, torch.float32, (T, K)), T, router,
-            _typed(dlogits, torch.float32, (T, N)))
-    _here(logits, ids, dw, dlogits)
-    rc = lib.exfold_route_backward(layer, *args, _stream(stream))
+    (T, N), K = logits.shape, layer.top_k
+    if not (logits.dtype is dw.dtype is dlogits.dtype is torch.float32 and ids.dtype is torch.int32 and N == layer.n_experts and
+            ids.shape == dw.shape == (T, K) and dlogits.shape == logits.shape and logits.is_contiguous() and ids.is_contiguous() and
+            dw.is_contiguous() and dlogits.is_contiguous()):
+        _typed(logits, torch.float32, (T, layer.n_experts)), _typed(ids, torch.int32, (T, K)), _typed(dw, torch.float32, (T, K))
+        _typed(dlogits, torch.float32, (T, N))
+    dev = torch._C._cuda_getDevice()
+    if not logits.get_device() == ids.get_device() == dw.get_device() == dlogits.get_device() == dev:
+        _here(logits, ids, dw, dlogits)
+    rc = lib.exfold_route_backward(layer, logits.data_ptr(), ids.data_ptr(), dw.data_ptr(), T, router, dlogits.data_ptr(),
+                                   stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(dev))
     if check and rc != 0:
         raise ExfoldError(rc, "exfold_route_backward")
     return rc
@@ -535,19 +546,26 @@ def exfold_linear(x, w, y, ws, bias=None, residual=None, activation: str = "none
     """y = act(x w^T + bias) + residual. x [T][in], w [out][in], bias [out] of one type; y, residual [T][out]. The matrices may
     have any distance between their rows."""
     T, i = x.shape
-    o, dt, out, ldr = w.shape[0], x.dtype, y.dtype, 0
+    o, dt, out, ldr, rp, bp = w.shape[0], x.dtype, y.dtype, 0, None, None
     (ldx, sx), (ldw, sw), (ldy, sy) = x.stride(), w.stride(), y.stride()
     if not (sx == sw == sy == 1 and ldx >= i and ldw >= i and ldy >= o and w.shape[1] == i and w.dtype is dt and y.shape == (T, o)):
         ldx, ldw, ldy = _rows(x, dt, T, i), _rows(w, dt, o, i), _rows(y, out, T, o)  # matrices of one row or column, or not usable
     if residual is not None:
-        ldr = _rows(residual, out, T, o)
-    if bias is not None and (bias.dtype is not dt or bias.shape != (o,) or not bias.is_contiguous()):
-        raise AssertionError(f"expected bias {dt} {(o,)}, got {bias.dtype} {tuple(bias.shape)}")
-    _here(x, w, bias, residual, y, ws)
+        ldr, sr = residual.stride()
+        if not (sr == 1 and ldr >= o and residual.dtype is out and residual.shape == y.shape):
+            ldr = _rows(residual, out, T, o)
+        rp = residual.data_ptr()
+    if bias is not None:
+        if bias.dtype is not dt or bias.shape != (o,) or not bias.is_contiguous():
+            raise AssertionError(f"expected bias {dt} {(o,)}, got {bias.dtype} {tuple(bias.shape)}")
+        bp = bias.data_ptr()
+    dev = torch._C._cuda_getDevice()
+    if not (x.get_device() == w.get_device() == y.get_device() == ws.get_device() == dev and (bp is None or bias.get_device() == dev) and
+            (rp is None or residual.get_device() == dev)):
+        _here(x, w, bias, residual, y, ws)
     rc = lib.exfold_linear(_linear_desc(i, o, _LINEAR_DTYPES[dt], _LINEAR_DTYPES[out], ACTIVATIONS[activation], ldx, ldw, ldy, ldr),
-                           x.data_ptr(), w.data_ptr(), bias.data_ptr() if bias is not None else None,
-                           residual.data_ptr() if residual is not None else None, T, y.data_ptr(), ws.data_ptr(), ws.numel(),
-                           _stream(stream))
+                           x.data_ptr(), w.data_ptr(), bp, rp, T, y.data_ptr(), ws.data_ptr(), ws.numel(),
+                           stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(dev))
     if check and rc != 0:
         raise ExfoldError(rc, "exfold_linear")
     return rc
