@@ -271,3 +271,14 @@ def test_linear_kernels_beside_each_other(ex):
     torch.cuda.synchronize()
     for x, w, y, ws, r, alone, _ in jobs:
         assert ex.exfold_device_status(ws) == 0 and torch.equal(y, alone)
+
+
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("o", [4097, 4098, 4099, 4100, 4101, 4102, 4103, 4104, 4112, 4120])
+@pytest.mark.parametrize("T,i", [(2001, 512), (3001, 200)])
+def test_linear_pairs_write_nothing_behind_the_columns(ex, T, i, o, out):
+    """Rows whose distance suits a tensor map but whose length does not: what lies between them is the caller's."""
+    gap = (o + 7) // 8 * 8 + 16
+    check(ex, T, i, o, out=out, act="relu", ldy=gap, ldr=gap + 8)
+    check(ex, T, i, o, out=out, residual=False, ldy=gap)
+    check(ex, T, i, o, out=out, bias=False, in_place=True, ldy=gap)
