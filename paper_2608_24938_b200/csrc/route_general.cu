@@ -30,7 +30,8 @@ namespace {
 
 constexpr int kGrThreads = 256;
 constexpr float kMaskedScore = -3.402823466e38f;  // this and -infinity
-constexpr float kErrSigmoid = 2.f * 6.5f / (1 << 24), kErrSoftmax = 2.f * 22.f / (1 << 24), kErrChoice = 2.f / (1 << 24);
+constexpr float kRounding = 1.f / (1 << 24);
+constexpr float kErrSigmoid = 2.f * 6.5f * kRounding, kErrSoftmax = 2.f * 22.f * kRounding, kErrChoice = 2.f * kRounding;
 
 // Order-preserving image of a double; every NaN is the largest, -0 is +0
 __device__ __forceinline__ unsigned long long order64(double c) {
@@ -72,7 +73,7 @@ __device__ __forceinline__ int rank_exact(const RouteGeneralParams& p, const flo
     return out;
 }
 
-// One token's experts from 64-bit choices: lane k < K returns the k-th. cand: this lane's experts; sk: scratch of N words of the warp.
+// One token's experts from 64-bit choices: lane k < K returns the k-th. sk: scratch of N words of the warp.
 template <int NPL>
 __device__ __forceinline__ int pick_exact(const RouteGeneralParams& p, const float* z, unsigned long long* sk, int lane) {
     const int N = p.N, K = p.K;
@@ -179,7 +180,23 @@ __device__ __forceinline__ bool pick_groups(const RouteGeneralParams& p, unsigne
         k2 = max(min(k1, a), max(k2, b));
         k1 = max(k1, a);
     }
-    if (p.group_top2 && k2 > order32(-INFINITY)) k1 = order32(from_order32(k1) + from_order32(k2));
+    // The group's value lies between lower and upper in 64 bits: a choice is off by its score's error and a rounding of its own size, the
+    // sum of two by both and one of its own. (Choices of opposite signs are far larger than their sum, and so are their roundings.)
+    unsigned lower = k1, upper = k1;  // a masked or a NaN group is what it is
+    const float c1 = from_order32(k1);
+    if (c1 > -INFINITY) {
+        const float score_off = (p.softmax ? kErrSoftmax : kErrSigmoid) * 0.5f;
+        float value = c1, off = score_off + kRounding * fabsf(c1);
+        if (p.group_top2 && k2 > order32(-INFINITY)) {
+            const float c2 = from_order32(k2);
+            value += c2;
+            off += score_off + kRounding * (fabsf(c2) + fabsf(value));
+            k1 = order32(value);
+        }
+        off = 1.01f * off + kRounding * fabsf(value);  // with the roundings of these lines
+        lower = isinf(off) ? order32(-INFINITY) : order32(value - off);  // the sum overflowed: anywhere
+        upper = isinf(off) ? 0xffffffffu : order32(value + off);
+    }
     if (g >= G) k1 = 0;
     int place = 0;
     for (int o = 0; o < G; ++o) {
@@ -188,11 +205,11 @@ __device__ __forceinline__ bool pick_groups(const RouteGeneralParams& p, unsigne
     }
     const bool in = g < G && place < p.top_groups;
     const unsigned stay = __ballot_sync(0xffffffffu, in);
-    const unsigned last = __reduce_min_sync(0xffffffffu, in ? k1 : 0xffffffffu), next = __reduce_max_sync(0xffffffffu, in ? 0u : k1);
+    const unsigned last = __reduce_min_sync(0xffffffffu, in ? lower : 0xffffffffu), next = __reduce_max_sync(0xffffffffu, in || g >= G ? 0u : upper);
 #pragma unroll
     for (int q = 0; q < NPL; ++q)
         if (!((stay >> min(31, (lane + 32 * q) / per * lanes)) & 1u)) key[q] = 0;
-    return !p.by_score || !close_call(from_order32(last), from_order32(next), 2.f * (p.softmax ? kErrSoftmax : kErrSigmoid));
+    return !p.by_score || last > next || next == order32(-INFINITY);  // (every group left out is masked: those go by their places)
 }
 
 // Descending; neighbours change places only if the second is larger, so equal keys stay in the order of their experts

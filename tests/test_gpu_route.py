@@ -377,3 +377,34 @@ def test_route_beyond_32_bit_offsets(ex):
     bound = grad_bound(tail, rid, g[-5:].cpu().numpy(), "softmax", True, 1.0)
     assert bool((np.abs(dz[-5:].cpu().numpy() - ref) <= bound).all())
     assert torch.equal(dz[:-5].amax(0)[:2].cpu(), torch.tensor([0.5, -0.5])) and torch.equal(dz[:-5, 2:].abs().amax(), dz.new_zeros(()))
+
+
+def tied_groups(T, N, G, plus, minus, amp, seed):
+    """Scores and a bias whose groups' two largest choices are s + plus and s + minus, with sums `amp` times a few fp32 roundings apart:
+    every group has the same scores but for small differences."""
+    rng = np.random.default_rng(seed)
+    per = N // G
+    z = np.tile(rng.standard_normal((T, per)), (1, G)) + rng.uniform(-1, 1, (T, N)) * amp
+    bias = np.full((G, per), minus, np.float32)
+    bias[:, 0] = plus
+    return z.astype(np.float32), bias.ravel()
+
+
+@pytest.mark.parametrize("score,slope", [("sigmoid", 0.2), ("softmax", 0.008)])
+@pytest.mark.parametrize("plus,minus", [(16, -16), (100, -100), (1000, -1000), (-100, 100), (1030, 1030), (-1030, -1030), (1000, 900),
+                                        (3e30, -3e30), (3e38, 3e38), (-3e38, -3e38)])
+@pytest.mark.parametrize("N,G,top,K", [(256, 8, 4, 8), (8, 2, 1, 1), (96, 3, 2, 5)])
+def test_route_groups_of_large_biases(ex, score, slope, plus, minus, N, G, top, K):
+    """Sums of two choices are rounded at the size of the choices, which may be far above the sum's."""
+    amp = min(0.5, max(abs(plus), abs(minus)) * 2.0 ** -22 / slope)
+    z, bias = tied_groups(300, N, G, plus, minus, amp, seed=int(abs(plus) % 1000) + N)
+    for group_score in ("top2", "max"):
+        check_route(ex, z, K, score=score, bias=bias, n_groups=G, top_groups=top, group_score=group_score)
+
+
+def test_route_groups_fp32_sums_are_in_the_wrong_order(ex):
+    """A token whose groups score 0.948400 and 0.948380, in fp32 0.948364 and 0.948425."""
+    z = np.array([[-1.704, -1.145, -0.586, 1.352, -1.632, 0.562, 1.294, 0.458]], np.float32)
+    bias = np.tile(np.array([1000, -1000, -1000, -1000], np.float32), 2)
+    assert route64(z, 1, "sigmoid", bias=bias, n_groups=2, top_groups=1, group_score="top2")[0][0, 0] == 0
+    check_route(ex, z, 1, score="sigmoid", bias=bias, n_groups=2, top_groups=1, group_score="top2")
