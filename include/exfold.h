@@ -197,7 +197,7 @@ int exfold_moe_prefill(const exfold_layer *layer, const void *x, const float *lo
  *                     not positive).
  *   confidence_split  != 0: with c = clip(1 - L[s][t], 0, 1) for the minimum-loss target t, the part
  *                     w_s c S[s][t] is folded onto t and w_s (1 - c) is spread over the retained
- *                     routes in proportion to their original router weights.
+ *                     routes in proportion to their original router weights (equally where those sum to 0).
  *   gemm_path         0: the library chooses the tensor-core kernels (above); 1: one-CTA kernel only;
  *                     2: CTA pairs wherever a group has a pair of row tiles; 3: the one pass over whole and
  *                     ragged tiles. Same results bit for bit.

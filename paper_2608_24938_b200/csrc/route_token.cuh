@@ -72,7 +72,8 @@ __device__ __forceinline__ TokenRoute fold_token(const PrefillRouteParams& p, in
                     const unsigned tm = __ballot_sync(0xffffffffu, is_t);
                     const float lt = __shfl_sync(0xffffffffu, lv[u], __ffs(tm) - 1);
                     c = fminf(fmaxf(1.0f - lt, 0.0f), 1.0f);
-                    if (kept) wt = __fadd_rn(wt, ws * (1.0f - c) * (w / kept_sum));
+                    // retained routes that weigh nothing (a masked token's given routes, an expert of norm 0 omitted) share equally
+                    if (kept) wt = __fadd_rn(wt, ws * (1.0f - c) * (kept_sum != 0.f ? w / kept_sum : 1.0f / (float)Kp));
                 }
                 if (is_t) wt = __fadd_rn(wt, __fmul_rn(ws * c, sv[u]));
             }

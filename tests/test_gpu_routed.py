@@ -281,3 +281,46 @@ def test_block_from_hidden_states_under_capture(ex):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(first, (hid, logits, ids, w, y, out)))
+
+
+@pytest.mark.parametrize("name", ["tiny", "f32_shared", "bf16_shared"])
+@pytest.mark.parametrize("opts", [dict(), dict(rescale=True), dict(loss_threshold=0.7), dict(loss_threshold=0.7, rescale=True)])
+@pytest.mark.parametrize("T", [4, 30, 300])
+def test_confidence_split_over_weights_of_zero(ex, name, opts, T):
+    """Retained routes that all weigh 0 share what is spread equally: nothing is lost, and nothing is divided by their sum."""
+    cfg = CONFIGS[name]
+    N, K = cfg.n_experts, cfg.top_k
+    Kp = (K + 1) // 2
+    case = Case(dataclasses.replace(cfg, calib_tokens=0), T=T)
+    S, L, h, _ = (t.copy() for t in case.np_tables())
+    h[N - 1] = 0.0  # never retained before another
+    with np.errstate(divide="ignore"):
+        case.set_tables((S, L, h, np.log(h)))
+    ids, w = routes(cfg, T, seed=6)
+    given = ids.copy()
+    given[0], ids[0], w[0] = -1, 0, 0.0  # no expert at all: expert 0, K times
+    w[1] = 0.0
+    ids[2] = given[2] = [*range(K - 1), N - 1]
+    w[2] = [0.0] * (K - 1) + [1.25]
+    some = np.arange(T) >= 3
+    ri, rw = np.zeros((T, Kp), np.int32), np.zeros((T, Kp))
+    if some.any():
+        ri[some], rw[some] = fold64(ids[some], w[some], Kp, S, L, h, opts.get("loss_threshold", np.inf), opts.get("rescale", False), True)[:2]
+    ri[1] = np.sort(ids[1])[:Kp]
+    ri[2] = ids[2, :Kp]
+    adm = [t for t in ri[2] if not L[N - 1, t] > opts.get("loss_threshold", np.inf)]
+    if adm:
+        t = min(adm, key=lambda e: (L[N - 1, e], e))
+        c = min(max(1.0 - float(L[N - 1, t]), 0.0), 1.0)
+        rw[2] = 1.25 * (1 - c) / Kp
+        rw[2, list(ri[2]).index(t)] += 1.25 * c * float(S[N - 1, t])
+        if opts.get("rescale") and rw[2].sum() > 0:
+            rw[2] *= 1.25 / rw[2].sum()
+    y, m = run_prefill(case, case.x, given, w, Kp, confidence_split=True, **opts)
+    assert np.array_equal(m["ids"], ri)
+    np.testing.assert_allclose(m["w"], rw, rtol=2e-5, atol=2e-6)
+    clean = ri.copy()
+    clean[0] = np.arange(Kp)  # different experts for the oracle; they weigh 0
+    check_output(y, experts(case, case.x, clean, rw), cfg.dtype)
+    bare, _ = run_prefill(case, case.x, given, w, Kp, meta=False, confidence_split=True, **opts)
+    assert np.array_equal(bare, y)
