@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(kThreads, 2) decode_small_gateup_kernel(Decode
             const int e = ids[s];
             sc.in_union[e] = 1;
             if (GIVEN) continue;
-            const unsigned long long fx = (unsigned long long)(w64[s] * 9007199254740992.0);
+            const unsigned long long fx = pool_units(w64[s]);
             atomicAdd(&sc.acc32[3 * e], (unsigned)(fx & 0x1FFFFFull));
             atomicAdd(&sc.acc32[3 * e + 1], (unsigned)((fx >> 21) & 0x1FFFFFull));
             atomicAdd(&sc.acc32[3 * e + 2], (unsigned)(fx >> 42));
@@ -216,9 +216,7 @@ __global__ void __launch_bounds__(kThreads, 2) decode_small_gateup_kernel(Decode
         if (!GIVEN && (U > p.M || p.pool_ids != nullptr)) {
             // pool = best M experts of the union by (score desc, id asc): rank by counting over the members
             if (is_member) {
-                const unsigned long long acc = (unsigned long long)sc.acc32[3 * tid] +
-                                               ((unsigned long long)sc.acc32[3 * tid + 1] << 21) +
-                                               ((unsigned long long)sc.acc32[3 * tid + 2] << 42);
+                const unsigned long long acc = pool_sum(&sc.acc32[3 * tid]);
                 sc.key[mine] = score_order_key((double)acc * (1.0 / 9007199254740992.0) * (double)h_e);
             }
             __syncthreads();

@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(kFThreads, 1) decode_ffn_kernel(const __grid_c
     auto add_slot = [&](int id, double wv) {
         // The routed weight in 2^-53 fixed point, added as three 21-bit limbs with 32-bit integer atomics (at most 256
         // addends per expert, so no limb overflows): exact, and independent of the order of arrival.
-        const unsigned long long fx = (unsigned long long)(wv * 9007199254740992.0);
+        const unsigned long long fx = pool_units(wv);
         atomicAdd(&sc.acc32[3 * id], (unsigned)(fx & 0x1FFFFFull));
         atomicAdd(&sc.acc32[3 * id + 1], (unsigned)((fx >> 21) & 0x1FFFFFull));
         atomicAdd(&sc.acc32[3 * id + 2], (unsigned)(fx >> 42));
@@ -339,9 +339,7 @@ __global__ void __launch_bounds__(kFThreads, 1) decode_ffn_kernel(const __grid_c
             const unsigned m = __ballot_sync(0xffffffffu, in);
             if (in && c % (kFThreads / 32) == warp) {
                 const int pos = U + __popc(m & ((1u << lane) - 1u));
-                const unsigned long long acc = (unsigned long long)sc.acc32[3 * e] +
-                                               ((unsigned long long)sc.acc32[3 * e + 1] << 21) +
-                                               ((unsigned long long)sc.acc32[3 * e + 2] << 42);
+                const unsigned long long acc = pool_sum(&sc.acc32[3 * e]);
                 const long long key =
                     score_order_key((double)acc * (1.0 / 9007199254740992.0) * (double)(c < kFThreads / 32 ? h_e[0] : h_e[1]));
                 member[pos] = e;

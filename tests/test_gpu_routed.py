@@ -324,3 +324,34 @@ def test_confidence_split_over_weights_of_zero(ex, name, opts, T):
     check_output(y, experts(case, case.x, clean, rw), cfg.dtype)
     bare, _ = run_prefill(case, case.x, given, w, Kp, meta=False, confidence_split=True, **opts)
     assert np.array_equal(bare, y)
+
+
+@pytest.mark.parametrize("name", ["tiny", "f32_shared", "bf16", "bf16_shared"])
+@pytest.mark.parametrize("B", [1, 8, 9, 200, 256])
+def test_decode_routed_weights_of_any_size(ex, name, B):
+    """Pool sums neither wrap where an expert's weights sum to 2048 and more nor take a negative or NaN weight for a large one."""
+    cfg = CONFIGS[name]
+    case = Case(dataclasses.replace(cfg, calib_tokens=0), B=B)
+    S, L, h, _ = case.np_tables()
+    N, K = cfg.n_experts, cfg.top_k
+    ids, w = routes(cfg, B, seed=7)
+    ids[:, 0], ids[:, 1] = 5, 6
+    for i in range(B):
+        ids[i, 2:] = np.random.default_rng(i).permutation([e for e in range(N) if e not in (5, 6)])[:K - 2]
+    w[:, 0], w[:, 1] = 2100.0 / B, 400.0 / B  # a sum of 2100: 52 where it wraps
+    w = w.astype(np.float32)
+    def pools(weights, counted):
+        for M in (1, 2):
+            pool, target, scale, ri, rw = pool64(ids, counted, M, S, L, h)
+            y, m = run_decode(case, case.xd, ids, weights, M)
+            assert m["pool_ids"][:len(pool)].tolist() == pool
+            assert np.array_equal(m["ids"], ri) and np.array_equal(m["target"], target)
+            if np.isfinite(weights).all():
+                check_output(y, experts(case, case.xd, ri, weights.astype(np.float64) * scale[ids]), cfg.dtype)
+    pools(w, w)
+    w[:, 0] *= np.float32(1e4)
+    pools(w, w)
+    for bad in (-3.0, -1e10, np.nan):
+        v = w.copy()
+        v[:, 0] = bad
+        pools(v, np.where(v > 0, v, np.float32(0.0)))
