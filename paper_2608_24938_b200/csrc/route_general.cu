@@ -18,7 +18,7 @@
 // quotient 4: below 22. And the addition's half step of the choice. Two choices are sure of their order if further apart than twice that.
 //
 // GPU time, 64-bit choices for every token -> now (sigmoid, bias, Top-8): 16384 tokens x 128 experts 23.2 -> 10.6 us, 777 x 256 in 8 groups
-// with the load 13.2 -> 6.3, one token 4.4 -> 2.5; gradient, a token per warp -> now: 16384 x 128 13.0 -> 3.8, softmax over all experts 6.9.
+// with the load 13.2 -> 6.3, one token 4.4 -> 2.5; gradient, a token per warp -> now: 16384 x 128 13.0 -> 3.8, softmax over all experts 6.3.
 // Ranking by one word (24 bits of the choice, 8 of the expert: one reduction per round instead of two) took 12.1 and 6.9 us (blocks of 256 threads: 12.8 and 5.9).
 #include <algorithm>
 
@@ -392,16 +392,28 @@ __global__ void __launch_bounds__(route_threads(NPL)) route_general_kernel(const
     }
 }
 
-// The gradient, up to `batch` <= 32 / SLOTS tokens of a warp at a time: lane SLOTS t + k holds token t's chosen expert k. Rows are written
+// Tokens of a warp at a time. The rows of four tokens of more than 128 experts do not fit the registers of four blocks per SM (16384 x 256,
+// softmax over all: 10.6 us, with two 9.7).
+__host__ __device__ constexpr int back_batch(int nq, int slots, bool dense) { return dense && nq > 1 && slots < 16 ? 2 : 32 / slots; }
+
+// The gradient, up to `batch` <= back_batch tokens of a warp at a time: lane SLOTS t + k holds token t's chosen expert k. Rows are written
 // without the chosen ones (zeros, or the softmax over all experts), and those after them. VEC: rows of whole, aligned groups of four,
 // expert 4 lane + j + 128 q in v[q][j]; else expert lane + 32 (4 q + j). A row is 4 N bytes written, and as many read where the softmax is
 // over all experts.
-template <int NQ, int SLOTS, bool VEC>
-__global__ void __launch_bounds__(kGrThreads) route_backward_kernel(const __grid_constant__ RouteBackwardParams p) {
-    constexpr int kBatch = 32 / SLOTS;
+//
+// Softmax over all experts, R the sum of exp(z - max) over the experts that were not chosen, e_k those of the chosen, E = R + sum e_k:
+// a chosen one gets s_k (g_k R + sum_j (g_k - g_j) e_j) / E, any other -s sum_j g_j e_j / E. A confident router's s_k is close to 1, and as
+// g_k s_k - s_k sum_j g_j s_j its entry would be what is left of two nearly equal numbers. R is an fp32 sum of its own terms; the e_j and
+// their sums are 64-bit ones, one lane per slot.
+// DENSE: softmax over all experts.
+template <int NQ, int SLOTS, bool VEC, bool DENSE>
+__global__ void __launch_bounds__(kGrThreads, 4) route_backward_kernel(const __grid_constant__ RouteBackwardParams p) {
+    constexpr int kBatch = back_batch(NQ, SLOTS, DENSE);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = (int)blockDim.x >> 5;
     const int N = p.N, K = p.K, batch = p.batch;
-    const bool dense = p.softmax && !p.renormalise;
+    constexpr int kWords = kMaxExperts / 32;
+    __shared__ unsigned s_chosen[DENSE ? kGrThreads / 32 : 1][kBatch * kWords];  // bits of each token's chosen experts
+    unsigned* chosen = s_chosen[DENSE ? warp : 0];
     auto expert = [&](int q, int j) { return VEC ? 4 * lane + 128 * q + j : lane + 32 * (4 * q + j); };
     grid_dep_launch();
     grid_dep_wait();
@@ -415,9 +427,13 @@ __global__ void __launch_bounds__(kGrThreads) route_backward_kernel(const __grid
         const float g = id >= 0 ? p.dw[i * K + k] : 0.f;
         const float zk = id >= 0 ? p.logits[i * N + id] : -INFINITY;
         const bool live = zk > kMaskedScore || isnan(zk);
-        float ex[kBatch][NQ][4];  // softmax over all experts: exp(z - max) of each token's experts
-        float my_max = 0.f, my_inv = 1.f, invs[kBatch];
-        if (dense) {
+        float ex[DENSE ? kBatch : 1][NQ][4];  // exp(z - max) of each token's experts
+        float my_max = 0.f, my_rest = 0.f;
+        if constexpr (DENSE) {
+            if (lane < kBatch * kWords) chosen[lane] = 0u;
+            __syncwarp();
+            if (id >= 0) atomicOr(&chosen[t * kWords + (id >> 5)], 1u << (id & 31));
+            __syncwarp();
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
                 if (u >= here) break;
@@ -437,31 +453,35 @@ __global__ void __launch_bounds__(kGrThreads) route_backward_kernel(const __grid
                     for (int j = 0; j < 4; ++j) zmax = isnan(ex[u][q][j]) || ex[u][q][j] > zmax ? ex[u][q][j] : zmax;
                 }
                 zmax = from_order32(__reduce_max_sync(0xffffffffu, order32(zmax)));
-                float sum = 0.f;
+                float rest = 0.f;
 #pragma unroll
                 for (int q = 0; q < NQ; ++q)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
+                        const int e = expert(q, j);  // (of no expert: 0, whatever the bit)
                         ex[u][q][j] = ex[u][q][j] <= kMaskedScore ? 0.f : expf(ex[u][q][j] - zmax);
-                        sum += ex[u][q][j];
+                        rest += (chosen[u * kWords + ((e >> 5) & (kWords - 1))] >> (e & 31)) & 1u ? 0.f : ex[u][q][j];
                     }
 #pragma unroll
-                for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                invs[u] = 1.f / sum;
+                for (int o = 16; o > 0; o >>= 1) rest += __shfl_xor_sync(0xffffffffu, rest, o);
                 if (t == u) {
                     my_max = zmax;
-                    my_inv = invs[u];
+                    my_rest = rest;
                 }
             }
         }
-        float dz, dot = 0.f;  // of the chosen expert; dense: sum of the token's
-        if (dense) {
-            const float sk = live ? expf(zk - my_max) * my_inv : 0.f;
-            dz = live ? p.scale * g * sk : 0.f;
-            dot = dz;
+        float dz, others = 0.f;  // of the chosen expert; the other experts' as a factor of exp(z - max)
+        if constexpr (DENSE) {
+            const double e = live ? exp((double)zk - (double)my_max) : 0.0;
+            double sum = e, dot = e * (double)g;
 #pragma unroll
-            for (int o = SLOTS / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-            dz = live ? dz - dot * sk : 0.f;
+            for (int o = SLOTS / 2; o > 0; o >>= 1) {
+                sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                dot += __shfl_xor_sync(0xffffffffu, dot, o);
+            }
+            const double all = sum + (double)my_rest, inv = all != 0.0 ? 1.0 / all : 0.0, factor = (double)p.scale * inv * inv;
+            dz = live ? (float)(factor * e * ((double)g * (double)my_rest + ((double)g * sum - dot))) : 0.f;
+            others = (float)(-factor * dot);
         } else {
             double s = 0.0, rest = 1.0;  // score (softmax: up to a factor), 1 - score
             if (p.softmax) {
@@ -493,13 +513,16 @@ __global__ void __launch_bounds__(kGrThreads) route_backward_kernel(const __grid
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
             if (u >= here) break;
-            const float f = dense ? -__shfl_sync(0xffffffffu, dot, SLOTS * u) * invs[u] : 0.f;
+            const float f = DENSE ? __shfl_sync(0xffffffffu, others, SLOTS * u) : 0.f;
             float* dst = p.dlogits + (i0 + u) * N;
 #pragma unroll
             for (int q = 0; q < NQ; ++q) {
                 float o[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) o[j] = dense && ex[u][q][j] != 0.f ? f * ex[u][q][j] : 0.f;  // a masked expert has none
+                for (int j = 0; j < 4; ++j) {
+                    const float e = DENSE ? ex[DENSE ? u : 0][q][j] : 0.f;
+                    o[j] = e != 0.f ? f * e : 0.f;  // a masked expert has none
+                }
                 if (VEC) {
                     if (expert(q, 0) < N) *reinterpret_cast<float4*>(dst + expert(q, 0)) = make_float4(o[0], o[1], o[2], o[3]);
                 } else {
@@ -546,14 +569,17 @@ cudaError_t launch_route_backward(RouteBackwardParams p, int sms, cudaStream_t s
     if (p.T == 0) return cudaSuccess;
     constexpr int kWarps = kGrThreads / 32;
     const int slots = p.K <= 8 ? 8 : p.K <= 16 ? 16 : 32;
-    p.batch = p.T >= (int64_t)sms * kWarps * 4 ? 32 / slots : 1;
+    const bool dense = p.softmax && !p.renormalise;
+    p.batch = p.T >= (int64_t)sms * kWarps * 4 ? back_batch(p.N <= 128 ? 1 : 2, slots, dense) : 1;
     const unsigned blocks = (unsigned)std::min<int64_t>((p.T + kWarps * p.batch - 1) / (kWarps * p.batch), (int64_t)8 * sms);
     const bool vec = p.N % 4 == 0 && ((reinterpret_cast<uintptr_t>(p.logits) | reinterpret_cast<uintptr_t>(p.dlogits)) & 15) == 0;
     auto go = [&](auto kernel) { return launch_pdl(kernel, blocks, kGrThreads, 0, s, p); };
-#define EXFOLD_BACK(NQ, V) \
-    (slots == 8 ? go(route_backward_kernel<NQ, 8, V>) : slots == 16 ? go(route_backward_kernel<NQ, 16, V>) : go(route_backward_kernel<NQ, 32, V>))
+#define EXFOLD_BACK_D(NQ, V, D) \
+    (slots == 8 ? go(route_backward_kernel<NQ, 8, V, D>) : slots == 16 ? go(route_backward_kernel<NQ, 16, V, D>) : go(route_backward_kernel<NQ, 32, V, D>))
+#define EXFOLD_BACK(NQ, V) (dense ? EXFOLD_BACK_D(NQ, V, true) : EXFOLD_BACK_D(NQ, V, false))
     if (p.N <= 128) return vec ? EXFOLD_BACK(1, true) : EXFOLD_BACK(1, false);
     return vec ? EXFOLD_BACK(2, true) : EXFOLD_BACK(2, false);
+#undef EXFOLD_BACK_D
 #undef EXFOLD_BACK
 }
 

@@ -408,3 +408,42 @@ def test_route_groups_fp32_sums_are_in_the_wrong_order(ex):
     bias = np.tile(np.array([1000, -1000, -1000, -1000], np.float32), 2)
     assert route64(z, 1, "sigmoid", bias=bias, n_groups=2, top_groups=1, group_score="top2")[0][0, 0] == 0
     check_route(ex, z, 1, score="sigmoid", bias=bias, n_groups=2, top_groups=1, group_score="top2")
+
+
+def peaked_grad64(z, ids, g, scale):
+    """The gradient over all experts with 1 - s taken from the other experts' exponentials; and the sum of magnitudes of what each
+    entry is made of, once the terms that cancel exactly are gone."""
+    T, N = z.shape
+    s, _ = scores64(z.astype(np.float64), "softmax")
+    rows = np.arange(T)[:, None]
+    chosen = np.zeros((T, N), bool)
+    chosen[rows, ids] = True
+    G = np.zeros((T, N))
+    G[rows, ids] = g
+    sc = np.where(chosen, s, 0.0)
+    rest = np.where(chosen, 0.0, s).sum(1, keepdims=True)
+    diff = G[:, :, None] - G[:, None, :]  # [e][k]
+    value = np.where(chosen, G * rest + (diff * sc[:, None, :]).sum(2), -(G * sc).sum(1, keepdims=True)) * s * scale
+    terms = np.where(chosen, np.abs(G) * rest + (np.abs(diff) * sc[:, None, :]).sum(2), np.abs((G * sc).sum(1, keepdims=True))) * s * scale
+    return value, terms
+
+
+@pytest.mark.parametrize("N,K", [(64, 1), (64, 2), (128, 8), (33, 5), (200, 10), (256, 32)])
+@pytest.mark.parametrize("T", [7, 1300, 5000])
+def test_route_backward_of_confident_routers(ex, N, K, T):
+    """Softmax over all experts with one or two scores far above the others: what is left of a chosen expert's entry is small against
+    its own terms. The scores' exponentials are fp32 (argument |z - max|, 4 half steps of expf, 13 of the sum, 7 of products and
+    quotients, twice for a numerator and the sum), the chosen ones' and their sums 64-bit."""
+    T = min(T, 600000 // N // max(1, N // 32))
+    z = scores(T, N, seed=N + K)
+    top = np.random.default_rng(3).permutation(N)[:2]
+    z[:, top[0]] += np.linspace(0, 18, T, dtype=np.float32)
+    z[T // 2:, top[1]] = z[T // 2:, top[0]] - np.float32(0.25)
+    ids, _ = route64(z, K, "softmax", renormalise=False)
+    g = scores(T, K, seed=N + 2)
+    got = run_back(ex, z, ids, g, "softmax", False, 1.5)
+    ref, terms = peaked_grad64(z, ids, g, 1.5)
+    spread = (z.max(1, keepdims=True) - z).max()
+    bound = 2 * (spread + 4 + 13 + 7) * 2.0 ** -24 * terms + 1e-14 * 1.5 * np.abs(g).max() + 2.0 ** -126
+    bad = np.abs(got - ref) > bound
+    assert not bad.any(), f"{int(bad.sum())} entries, worst {float((np.abs(got - ref) / bound).max()):.1f} of the bound"
