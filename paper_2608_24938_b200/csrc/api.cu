@@ -1252,15 +1252,25 @@ static bool valid_linear(const exfold_linear_desc* d) {
 
 // bf16 rows that no tensor map takes are copied to rows of this many elements first
 static int64_t packed_row(const exfold_linear_desc* d) { return (d->in_features + 15) / 16 * 16; }
-static bool linear_packs(const exfold_linear_desc* d) {
-    return d->dtype == EXFOLD_BF16 && (((d->ldx ? d->ldx : d->in_features) | (d->ldw ? d->ldw : d->in_features)) & 7) != 0;
+// Rows of x and of w that the workspace has room to copy. A distance to a next row counts where there is one. Where either matrix lies
+// oddly both have room, so that the other may start anywhere; a single row always has, it may be cut from anywhere.
+struct LinearRoom {
+    int64_t x, w;
+    bool odd_x, odd_w;
+};
+static LinearRoom linear_room(const exfold_linear_desc* d, int64_t T) {
+    if (d->dtype != EXFOLD_BF16) return {};
+    const bool odd_x = T > 1 && ((d->ldx ? d->ldx : d->in_features) & 7) != 0;
+    const bool odd_w = d->out_features > 1 && ((d->ldw ? d->ldw : d->in_features) & 7) != 0;
+    if (odd_x || odd_w) return {T, d->out_features, odd_x, odd_w};
+    return {std::min<int64_t>(T, 1), d->out_features == 1 ? 1 : 0, false, false};
 }
+static size_t copied_bytes(const exfold_linear_desc* d, int64_t rows) { return align_up((size_t)packed_row(d) * 2 * rows, 256); }
 
 size_t exfold_linear_workspace_bytes(const exfold_linear_desc* desc, int64_t max_tokens) {
     if (!valid_linear(desc) || max_tokens < 0 || max_tokens > (int64_t)1 << 24) return 0;
-    if (!linear_packs(desc)) return sizeof(DeviceStatus);
-    return sizeof(DeviceStatus) + align_up((size_t)packed_row(desc) * 2 * max_tokens, 256) +
-           align_up((size_t)packed_row(desc) * 2 * desc->out_features, 256);
+    const LinearRoom room = linear_room(desc, max_tokens);
+    return sizeof(DeviceStatus) + copied_bytes(desc, room.x) + copied_bytes(desc, room.w);
 }
 
 int exfold_linear(const exfold_linear_desc* desc, const void* x, const void* w, const void* bias, const void* residual,
@@ -1277,17 +1287,28 @@ int exfold_linear(const exfold_linear_desc* desc, const void* x, const void* w, 
     p.ldx = desc->ldx ? desc->ldx : p.K; p.ldw = desc->ldw ? desc->ldw : p.K;
     p.ldy = desc->ldy ? desc->ldy : p.N; p.ldr = desc->ldr ? desc->ldr : p.N;
     if (residual == y && p.ldr != p.ldy && T > 1) return EXFOLD_ERR_INVALID_ARG;
-    if (ws_bytes < exfold_linear_workspace_bytes(desc, T)) return EXFOLD_ERR_WORKSPACE_TOO_SMALL;
+    LinearRoom room = linear_room(desc, T);
+    const bool odd = room.odd_x || room.odd_w, fits = ws_bytes >= exfold_linear_workspace_bytes(desc, T);
+    if (ws_bytes < sizeof(DeviceStatus) || (odd && !fits)) return EXFOLD_ERR_WORKSPACE_TOO_SMALL;
+    if (!fits) room.x = room.w = 0;  // a single row is read where it is
     if (T == 0) return EXFOLD_OK;
     p.status = at<DeviceStatus>(ws, 0);
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
     PdlScope pdl_scope(true);
-    if (linear_packs(desc)) {
+    const int64_t pitch = packed_row(desc);
+    if (T == 1) p.ldx = pitch;
+    if (p.N == 1) p.ldw = pitch;
+    bool copy_x = room.odd_x || (T <= room.x && !aligned16(x)), copy_w = room.odd_w || (p.N <= room.w && !aligned16(w));
+    if (!copy_w && !aligned16(w)) copy_x = false;  // the CUDA cores' in any case
+    if (!copy_x && !aligned16(x)) copy_w = false;
+    if (copy_w && T <= std::min<int64_t>(room.x, 8)) copy_x = true;  // next to nothing, and in_features then count as padded (linear_small_fits)
+    if (copy_x || copy_w) {
         char* xp = at<char>(ws, sizeof(DeviceStatus));
-        char* wp = xp + align_up((size_t)packed_row(desc) * 2 * T, 256);
-        EXFOLD_CUDA(launch_linear_pack(p, xp, wp, (int)packed_row(desc), sm_count(), s));
-        p.x = x = xp; p.w = w = wp;
-        p.K = (int)packed_row(desc); p.ldx = p.ldw = p.K;
+        char* wp = xp + copied_bytes(desc, room.x);
+        EXFOLD_CUDA(launch_linear_pack(p, copy_x ? xp : nullptr, copy_w ? wp : nullptr, (int)pitch, sm_count(), s));
+        if (copy_x) { p.x = x = xp; p.ldx = pitch; }
+        if (copy_w) { p.w = w = wp; p.ldw = pitch; }
+        if (copy_x && copy_w) p.K = (int)pitch;  // zeros behind in_features in both
     }
     if (bf16 && aligned16(x) && aligned16(w) && ((p.ldx | p.ldw) & 7) == 0) {
         if (linear_small_fits(p, sm_count())) {

@@ -493,7 +493,7 @@ struct LinearParams {
     DeviceStatus* status;  // cleared by the kernel, which is the call's first (or follows one that did)
 };
 cudaError_t launch_linear_simt(const LinearParams& p, bool bf16, bool out_bf16, int sms, cudaStream_t s);
-// Copies of x and w (bf16) with rows of `to` elements, zeros behind K (linear.cu)
+// Copies of x and w (bf16; those with a place for it) with rows of `to` elements, zeros behind K (linear.cu)
 cudaError_t launch_linear_pack(const LinearParams& p, void* xp, void* wp, int to, int sms, cudaStream_t s);
 // bf16, at most 8 tokens (linear_small.cu)
 bool linear_small_fits(const LinearParams& p, int sms);

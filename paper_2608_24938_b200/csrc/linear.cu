@@ -386,9 +386,9 @@ __global__ void __launch_bounds__(256) pack_rows_kernel(PackRows x, PackRows w, 
 }  // namespace
 
 cudaError_t launch_linear_pack(const LinearParams& p, void* xp, void* wp, int to, int sms, cudaStream_t s) {
-    const PackRows x{reinterpret_cast<const __nv_bfloat16*>(p.x), reinterpret_cast<__nv_bfloat16*>(xp), p.T, p.ldx};
-    const PackRows w{reinterpret_cast<const __nv_bfloat16*>(p.w), reinterpret_cast<__nv_bfloat16*>(wp), p.N, p.ldw};
-    const int64_t chunks = (p.T + p.N) * (to / 8);
+    const PackRows x{reinterpret_cast<const __nv_bfloat16*>(p.x), reinterpret_cast<__nv_bfloat16*>(xp), xp != nullptr ? p.T : 0, p.ldx};
+    const PackRows w{reinterpret_cast<const __nv_bfloat16*>(p.w), reinterpret_cast<__nv_bfloat16*>(wp), wp != nullptr ? p.N : 0, p.ldw};
+    const int64_t chunks = (x.rows + w.rows) * (to / 8);
     const unsigned grid = (unsigned)std::max<int64_t>(1, std::min<int64_t>((chunks + 255) / 256, (int64_t)16 * sms));
     return launch_pdl(pack_rows_kernel, grid, 256, 0, s, x, w, p.K, to, p.status);
 }

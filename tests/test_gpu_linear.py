@@ -282,3 +282,44 @@ def test_linear_pairs_write_nothing_behind_the_columns(ex, T, i, o, out):
     check(ex, T, i, o, out=out, act="relu", ldy=gap, ldr=gap + 8)
     check(ex, T, i, o, out=out, residual=False, ldy=gap)
     check(ex, T, i, o, out=out, bias=False, in_place=True, ldy=gap)
+
+
+@pytest.mark.parametrize("K", [4096, 520, 517])
+def test_linear_single_rows_of_wide_matrices(ex, K):
+    """The distance to a next row means nothing where there is none: one token, or one feature, cut from a matrix whose rows lie at
+    odd distances, on the workspace of dense rows."""
+    pad = (K + 7) // 8 * 8
+    for at in range(8):
+        wide = rows(9, K + 3 + K % 2, torch.bfloat16, 1 + at)[0]
+        row = wide[at:at + 1, :K]
+        many = rows(300, K, torch.bfloat16, 20, std=K ** -0.5, ld=pad)[0]
+        for T, o in ((1, 300), (1, 1), (5, 1), (300, 1)):
+            x, w = (row, many[:o]) if T == 1 else (many[:T], row)
+            ws = ex.alloc_linear_workspace(K, o, T, torch.bfloat16, ldx=0 if T == 1 else pad, ldw=0 if o == 1 else pad)
+            ws.fill_(0xFF)
+            r = rows(T, o, torch.bfloat16, 30)[0]
+            y = torch.full((T, o), float("nan"), dtype=torch.bfloat16, device="cuda")
+            ex.exfold_linear(x, w, y, ws, residual=r, activation="silu")
+            assert ex.exfold_device_status(ws) == 0
+            ref, bound = reference(x, w, None, r, "silu", torch.bfloat16)
+            assert ((y.double() - ref).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("K", [512, 517])
+@pytest.mark.parametrize("T,o", [(2, 600), (600, 3), (40, 300), (700, 520)])
+@pytest.mark.parametrize("odd", ["x", "w"])
+def test_linear_copies_only_what_lies_oddly(ex, K, T, o, odd):
+    pad = (K + 7) // 8 * 8
+    ld = K + 1 + K % 2  # odd
+    ldx, ldw = (ld, pad) if odd == "x" else (pad, ld)
+    x, w = rows(T, K, torch.bfloat16, 1, ld=ldx)[0], rows(o, K, torch.bfloat16, 2, std=K ** -0.5, ld=ldw)[0]
+    ws = ex.alloc_linear_workspace(K, o, T, torch.bfloat16, ldx=ldx, ldw=ldw)
+    ws.fill_(0xFF)
+    y = torch.full((T, o), float("nan"), dtype=torch.bfloat16, device="cuda")
+    ex.exfold_linear(x, w, y, ws)
+    assert ex.exfold_device_status(ws) == 0
+    ref, bound = reference(x, w, None, None, "none", torch.bfloat16)
+    assert ((y.double() - ref).abs() <= bound).all()
+    if T > 8 or odd == "x":  # (with few tokens their copy costs nothing)
+        copied = int((ws[256:] != 0xFF).sum())
+        assert copied <= (T if odd == "x" else o) * ((K + 15) // 16 * 32), "more than the one matrix was copied"

@@ -110,3 +110,18 @@ def test_binding_refuses_what_the_call_cannot_see(ex):
         ex.make_router(bias=torch.zeros(8, dtype=torch.float64))
     with pytest.raises(KeyError):
         ex.make_router("tanh")
+
+
+def test_linear_workspace_sizes(ex):
+    """Room for copies is asked for by what lies oddly, never less for more tokens, and a single row's distance counts nowhere."""
+    def size(t, i=4096, o=512, dt=1, ldx=0, ldw=0):
+        return ex.lib.exfold_linear_workspace_bytes(C.byref(ex.exfold_linear_desc(i, o, dt, dt, 0, ldx, ldw, 0, 0)), t)
+
+    row = 4096 * 2
+    assert size(1) == size(300) == size(1, ldx=4099) == 256 + row and size(300, dt=0) == 256
+    assert size(300, ldx=4099) == size(300, ldw=4099) == 256 + 812 * row
+    assert size(1, ldw=4099) == 256 + 513 * row
+    assert size(300, o=1) == size(300, o=1, ldw=4099) == 256 + 2 * row
+    for kw in (dict(), dict(ldx=4097), dict(ldw=4097), dict(i=4095), dict(o=1, ldx=4097), dict(dt=0)):
+        sizes = [size(t, **kw) for t in (0, 1, 2, 3, 9, 100)]
+        assert sizes == sorted(sizes)
