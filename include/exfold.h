@@ -363,11 +363,11 @@ int exfold_moe_decode_routed(const exfold_layer *layer, const void *x, const int
  * inputs; fp32 or bf16 for bf16). Sums, epilogue and activation in fp32, one rounding at the end. bias and residual may be
  * NULL. The ld fields are the distances between rows in elements (0: dense). residual may be y itself (the same rows and
  * distance); y overlaps no other operand.
- * Any sizes from 1 (in, out <= 2^24, T in [0, 2^24], T = 0 writes nothing). bf16 products run on the tensor cores: with ldx
- * and ldw multiples of 8 elements and x and w 16-byte aligned the operands are read in place; where a distance is no multiple
- * of 8, the matrix is first copied to aligned rows in the workspace, and so is the other one then if it does not start aligned, or a
- * single row (whose distance means nothing) that does not; other operands that only start unaligned, and fp32 ones, run on a
- * CUDA-core kernel.
+ * Any sizes from 1 (in, out <= 2^24, T in [0, 2^24]; T = 0 writes nothing, the status record neither: it stays what it was).
+ * bf16 products run on the tensor cores: with ldx and ldw multiples of 8 elements and x and w 16-byte aligned the operands are
+ * read in place; where a distance is no multiple of 8, the matrix is first copied to aligned rows in the workspace, and so is the
+ * other one then if it does not start aligned, or a single row (whose distance means nothing) that does not; other operands that
+ * only start unaligned, and fp32 ones, run on a CUDA-core kernel.
  * Results do not depend on other calls: no atomics, sums in a fixed order for the given sizes, distances and alignment.
  * Workspace: exfold_linear_workspace_bytes of the same description (256-byte aligned; its first 256 bytes are the status
  * record of exfold_device_status). Calls that share a workspace must be ordered on one stream.

@@ -539,7 +539,9 @@ def alloc_linear_workspace(in_features: int, out_features: int, max_tokens: int,
     n = exfold_linear_workspace_bytes(desc, max_tokens)
     if n == 0:
         raise ExfoldError(EXFOLD_ERR_INVALID_ARG, "exfold_linear_workspace_bytes")
-    return torch.empty(n, dtype=torch.uint8, device=device)
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    ws[:256].zero_()  # the status record: a call without tokens leaves it as it is
+    return ws
 
 
 def exfold_linear(x, w, y, ws, bias=None, residual=None, activation: str = "none", stream=None, check: bool = True) -> int:

@@ -323,3 +323,19 @@ def test_linear_copies_only_what_lies_oddly(ex, K, T, o, odd):
     if T > 8 or odd == "x":  # (with few tokens their copy costs nothing)
         copied = int((ws[256:] != 0xFF).sum())
         assert copied <= (T if odd == "x" else o) * ((K + 15) // 16 * 32), "more than the one matrix was copied"
+
+
+def test_linear_empty_call_leaves_everything(ex):
+    """No tokens: no output, no workspace is written, and a new workspace's status reads as no error."""
+    n = ex.alloc_linear_workspace(64, 8, 4, torch.bfloat16).numel()
+    stale = [torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda") for _ in range(8)]
+    torch.cuda.synchronize()
+    del stale  # the allocator hands these out again
+    for dtype in (torch.bfloat16, torch.float32):
+        w = torch.ones((8, 64), dtype=dtype, device="cuda")
+        ws = ex.alloc_linear_workspace(64, 8, 4, dtype)
+        assert ex.exfold_device_status(ws) == 0
+        ws[256:] = 0xFF
+        before, y = ws.clone(), torch.full((4, 8), 7.0, dtype=dtype, device="cuda")
+        ex.exfold_linear(w[:0], w, y[:0], ws, activation="relu")
+        assert ex.exfold_device_status(ws) == 0 and torch.equal(ws, before) and bool((y == 7).all())
