@@ -6,11 +6,32 @@
 
 namespace exfold {
 
+// In forms that keep their relative accuracy where they tend to 0 (1 + erf and 1 + tanh leave a result at -5 two digits).
+//
+// v Phi(v), Phi(-x) = 1/2 erfc(x / sqrt 2) = exp(-x^2 / 2) t P(t) with t = 1 / (1 + x / sqrt 8): erfc times exp(x^2) as a polynomial in
+// such a t is Hastings' form; this one (degree 8) was fitted for this file in equal ripples of the relative error, 4.3e-8 for x up
+// to 14, behind which exp underflows. 64 x 14336 x 4096 with erff 25.3 us, with erfcf 26.0, with this 25.2.
+__device__ __forceinline__ float linear_gelu(float v) {
+    const float t = __fdividef(1.0f, fmaf(fabsf(v), 0.353553391f, 1.0f));
+    float h = -0.0295346081f;
+    h = fmaf(h, t, 0.142288089f);
+    h = fmaf(h, t, -0.243601158f);
+    h = fmaf(h, t, 0.139034897f);
+    h = fmaf(h, t, -0.013313693f);
+    h = fmaf(h, t, 0.101343781f);
+    h = fmaf(h, t, 0.121551797f);
+    h = fmaf(h, t, 0.141187668f);
+    h = fmaf(h, t, 0.141043201f);
+    h *= t * exp2f(-0.721347520f * (v * v));
+    return v * (v < 0.f ? h : 1.0f - h);
+}
 __device__ __forceinline__ float linear_act(float v, int act) {
     switch (act) {  // uniform over the launch
         case EXFOLD_ACT_RELU: return v < 0.f ? 0.f : v;  // NaN stays
-        case EXFOLD_ACT_GELU: return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
-        case EXFOLD_ACT_GELU_TANH: return 0.5f * v * (1.0f + tanhf(0.79788456080286536f * (v + 0.044715f * v * v * v)));
+        case EXFOLD_ACT_GELU: return linear_gelu(v);
+        // 1/2 (1 + tanh u) = 1 / (1 + exp(-2 u)); an exponential above 2^126 makes the quotient 0. 777 x 1411 x 2040 with tanhf 14.5 us,
+        // with a rounded quotient 17.7, with this 14.5
+        case EXFOLD_ACT_GELU_TANH: return __fdividef(v, 1.0f + expf(-1.59576912f * fmaf(0.044715f * v, v * v, v)));
         case EXFOLD_ACT_SILU: return v / (1.0f + expf(-v));
         default: return v;
     }

@@ -339,3 +339,27 @@ def test_linear_empty_call_leaves_everything(ex):
         before, y = ws.clone(), torch.full((4, 8), 7.0, dtype=dtype, device="cuda")
         ex.exfold_linear(w[:0], w, y[:0], ws, activation="relu")
         assert ex.exfold_device_status(ws) == 0 and torch.equal(ws, before) and bool((y == 7).all())
+
+
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("dtype,T,i,o", [(torch.float32, 40, 1, 9), (torch.float32, 300, 3, 70), (torch.float32, 1024, 16, 2048),
+                                         (torch.bfloat16, 5, 64, 40), (torch.bfloat16, 300, 64, 264), (torch.bfloat16, 8192, 64, 5000)])
+def test_linear_activations_far_out(ex, act, dtype, T, i, o):
+    """Every activation in half steps of its own value, also where it tends to 0: one input counts, so that the sum is exact.
+    gelu: erfc to 4 steps, its argument to 3 half steps, which count (v^2 + 1) times; gelu_tanh and silu: v / (1 + e^-a), a to 8 half
+    steps (silu: exact), exp to 2 steps, the sum and the quotient to 4 half steps."""
+    v = torch.linspace(-9, 9, T).to(dtype)
+    x = torch.zeros((T, i), dtype=dtype)
+    x[:, i // 2] = v
+    w = torch.ones((o, i), dtype=dtype)
+    y = torch.full((T, o), float("nan"), device="cuda")
+    ws = ex.alloc_linear_workspace(i, o, T, dtype, torch.float32)
+    ex.exfold_linear(x.cuda(), w.cuda(), y, ws, activation=act)
+    assert ex.exfold_device_status(ws) == 0
+    d = v.double()
+    a = 2 * math.sqrt(2 / math.pi) * (d + 0.044715 * d ** 3)
+    ref = {"gelu": 0.5 * d * torch.special.erfc(-d / math.sqrt(2)), "gelu_tanh": d / (1 + torch.exp(-a)), "silu": d / (1 + torch.exp(-d))}[act]
+    steps = {"gelu": 8 + 3 * (d * d + 1) + 4, "gelu_tanh": 8 * a.abs() + 8 + 4, "silu": torch.full_like(d, 12.0)}[act]
+    bound = (steps * 2.0 ** -24 * ref.abs() + 2.0 ** -126)[:, None].cuda()
+    err = (y.double() - ref[:, None].cuda()).abs()
+    assert (err <= bound).all(), f"worst {float((err / bound).max()):.1f} of the bound"
