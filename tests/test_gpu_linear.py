@@ -363,3 +363,48 @@ def test_linear_activations_far_out(ex, act, dtype, T, i, o):
     bound = (steps * 2.0 ** -24 * ref.abs() + 2.0 ** -126)[:, None].cuda()
     err = (y.double() - ref[:, None].cuda()).abs()
     assert (err <= bound).all(), f"worst {float((err / bound).max()):.1f} of the bound"
+
+
+# Sizes that take the CTA pairs (linear_prefers_pairs), many of them with several items per pair or bands of row tiles
+PAIRS = [(2500, 1024, 2048), (6000, 72, 4099), (4096, 200, 2001), (8192, 4096, 2048), (1029, 4104, 4099), (300, 4096, 14336)]
+
+
+@pytest.mark.parametrize("T,i,o", PAIRS)
+def test_linear_pairs_results_and_residuals(ex, T, i, o):
+    """What the CTA-pair kernel does to its sums: results of both types, rows that a tensor map takes and rows that none does, with a
+    residual, without, and in place; K that ends inside a block, features that end inside 32 columns."""
+    p = (i + 7) // 8 * 8
+    p = dict(ldx=p, ldw=p)
+    even = (o + 7) // 8 * 8 + 8
+    check(ex, T, i, o, out=torch.float32, act="gelu", **p, ldy=even, ldr=even)
+    check(ex, T, i, o, out=torch.float32, act="relu", residual=False, **p, ldy=even)
+    check(ex, T, i, o, out=torch.float32, **p, ldy=o + 1 + o % 2, ldr=o + 3 + o % 2)
+    check(ex, T, i, o, act="silu", residual=False, **p, ldy=even)
+    check(ex, T, i, o, act="gelu_tanh", bias=False, **p, ldy=even, ldr=even)
+    check(ex, T, i, o, **p, ldy=o + 1 + o % 2, ldr=o + 3 + o % 2)
+    check(ex, T, i, o, residual=False, **p, ldy=o + 1 + o % 2)
+
+
+@pytest.mark.parametrize("T,i,o", PAIRS)
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+def test_linear_pairs_in_place(ex, T, i, o, out):
+    p = (i + 7) // 8 * 8
+    even = (o + 7) // 8 * 8
+    check(ex, T, i, o, out=out, in_place=True, act="relu", ldx=p, ldw=p, ldy=even)
+    check(ex, T, i, o, out=out, in_place=True, ldx=p, ldw=p, ldy=o + 1 + o % 2)
+
+
+BIG = [(1000, 100, 2048), (1300, 768, 1411), (500, 258, 2048), (1300, 203, 768), (500, 500, 1000), (1300, 768, 333), (300, 500, 768),
+       (1000, 507, 255), (128, 1411, 2048)]
+
+
+@pytest.mark.parametrize("dtype,out", [(torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32)])
+@pytest.mark.parametrize("T,i,o", BIG)
+def test_linear_large_cuda_core_tiles(ex, dtype, out, T, i, o):
+    """The 128 x 128 tiles on the CUDA cores, with K in 1, 2, 4 and 8 parts: fp32 and bf16 that only starts unaligned, rows in fours and not."""
+    offset = 0 if dtype == torch.float32 else 4
+    unit = 4 if dtype == torch.float32 else 8
+    ld = (i + unit - 1) // unit * unit
+    check(ex, T, i, o, dtype, out, act="silu", offset=offset, ldx=ld, ldw=ld)
+    check(ex, T, i, o, dtype, out, bias=False, offset=1, ldx=ld, ldw=ld, ldy=o + 3, ldr=o + 1)
+    check(ex, T, i, o, dtype, out, residual=False, offset=offset, ldx=ld, ldw=ld, ldy=o + 2)
