@@ -355,3 +355,26 @@ def test_decode_routed_weights_of_any_size(ex, name, B):
         v = w.copy()
         v[:, 0] = bad
         pools(v, np.where(v > 0, v, np.float32(0.0)))
+
+
+@pytest.mark.parametrize("name", list(CONFIGS))
+@pytest.mark.parametrize("T", [1, 8, 30, 200, 2100])
+def test_every_route_names_one_expert(ex, name, T):
+    """All rows are one expert's: K times as many as there are tokens (prefill), one per token (decode)."""
+    cfg = CONFIGS[name]
+    case = Case(dataclasses.replace(cfg, calib_tokens=0), T=T, B=min(T, 200))
+    K = cfg.top_k
+    ids, w = np.full((T, K), 3, np.int32), routes(cfg, T, seed=8)[1]
+    one = np.full((T, 1), 3, np.int32)
+    total = w.astype(np.float64).sum(1, keepdims=True)
+    y, m = run_prefill(case, case.x, ids, w, K)
+    assert (m["ids"] == 3).all()
+    check_output(y, experts(case, case.x, one, total), cfg.dtype)
+    bad = np.where(np.arange(K)[None, :] % 2 == 0, -1, cfg.n_experts).astype(np.int32).repeat(T, 0)
+    y, m = run_prefill(case, case.x, bad, w, K)  # no expert at all: expert 0 with weights of 0
+    assert (m["ids"] == 0).all() and (m["w"] == 0).all()
+    check_output(y, experts(case, case.x, one, total * 0), cfg.dtype) if cfg.n_shared else np.testing.assert_array_equal(y, 0)
+    B = case.B
+    y, m = run_decode(case, case.xd, ids[:B], w[:B], cfg.n_experts)
+    assert m["pool_size"][0] == 1 and m["pool_ids"][0] == 3
+    check_output(y, experts(case, case.xd, one[:B], total[:B]), cfg.dtype)
