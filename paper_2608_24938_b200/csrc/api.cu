@@ -1188,7 +1188,7 @@ int exfold_route(const exfold_layer* layer, const float* logits, int64_t T, cons
     p.n_groups = router->top_groups == G ? 1 : G;  // all groups stay: no groups
     p.top_groups = router->top_groups;
     p.group_top2 = router->group_score == EXFOLD_GROUP_TOP2 && N / G > 1;
-    p.by_score = router->bias != nullptr || (p.n_groups > 1 && p.group_top2);
+    p.by_score = router->bias != nullptr || (p.n_groups > 1 && router->group_score == EXFOLD_GROUP_TOP2);
     p.renormalise = router->renormalise != 0; p.scale = router->scale;
     p.ids = ids; p.w = w; p.load = load;
     PdlScope pdl_scope(true);

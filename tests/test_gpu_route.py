@@ -447,3 +447,12 @@ def test_route_backward_of_confident_routers(ex, N, K, T):
     bound = 2 * (spread + 4 + 13 + 7) * 2.0 ** -24 * terms + 1e-14 * 1.5 * np.abs(g).max() + 2.0 ** -126
     bad = np.abs(got - ref) > bound
     assert not bad.any(), f"{int(bad.sum())} entries, worst {float((np.abs(got - ref) / bound).max()):.1f} of the bound"
+
+
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+def test_route_groups_of_one_expert(ex, score):
+    """Groups that go by a sum of two rank by scores as others do, also where a group has one expert: sigmoids that are 1 in 64 bits tie."""
+    for N, top, K in ((8, 3, 2), (32, 7, 7), (32, 1, 1)):
+        z = np.concatenate([scores(20, N, seed=41), scores(20, N, seed=42, std=30.0), 40 + np.abs(scores(20, N, seed=43, std=5.0))])
+        for group_score in ("top2", "max"):
+            check_route(ex, z.astype(np.float32), K, score=score, n_groups=N, top_groups=top, group_score=group_score)
