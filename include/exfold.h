@@ -343,8 +343,8 @@ int exfold_route_backward(const exfold_layer *layer, const float *logits, const 
  * A token's K experts are different ones, in any order. An id outside [0, N) counts as expert 0 with weight 0.
  * Prefill (Eq. 10): routes are ranked by w h (one fp32 product; ties -> lower id) and keep their given weights; opts as in
  * exfold_moe_prefill_ex. With k_pre = K `tables` may be NULL (nothing is folded; slots are ranked by w).
- * Decode (Eq. 11): pool scores are h_e times the sum of the given weights. In these sums a negative weight and NaN count as 0, and a
- * sum of 2048 and more counts as 2048 (y is computed with the weights as they are).
+ * Decode (Eq. 11): pool scores are h_e times the sum of the given weights. In these sums a weight counts as at least 0 (NaN as 0)
+ * and at most 2048; y is computed with the weights as they are.
  */
 int exfold_moe_prefill_routed(const exfold_layer *layer, const void *x, const int32_t *ids, const float *w, int64_t T,
                               const void *w_gate, const void *w_up, const void *w_down, const exfold_tables *tables,

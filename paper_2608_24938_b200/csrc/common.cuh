@@ -79,12 +79,13 @@ __device__ __forceinline__ long long score_order_key(double score) {
     return b < 0 ? b ^ 0x7FFFFFFFFFFFFFFFll : b;            // negative: larger magnitude = smaller
 }
 // Weights are summed for the pool (Eq. 11) in units of 2^-53, exactly and in any order. Given weights may be anything: a negative one and
-// NaN count as 0, one of 2048 and more and a sum of that size as 2048, so that nothing wraps.
+// NaN count as 0, one of 2048 and more as 2048.
 __device__ __forceinline__ unsigned long long pool_units(double w) { return w > 0.0 ? __double2ull_rz(w * 9007199254740992.0) : 0ull; }
-// A sum kept as three 21-bit limbs (the top one holds what is left) in 32-bit words
-__device__ __forceinline__ unsigned long long pool_sum(const unsigned* limb) {
-    const unsigned long long low = (unsigned long long)limb[0] + ((unsigned long long)limb[1] << 21), high = (unsigned long long)limb[2] + (low >> 42);
-    return (high >> 22) != 0 ? ~0ull : (high << 42) | (low & ((1ull << 42) - 1));
+// A sum of up to 256 weights kept as three limbs in 32-bit words, of 21, 21 and 22 bits per weight; rounded once
+__device__ __forceinline__ double pool_sum(const unsigned* limb) {
+    const unsigned long long low = (unsigned long long)limb[0] + ((unsigned long long)limb[1] << 21);
+    const unsigned long long high = (unsigned long long)limb[2] + (low >> 42);  // below 2^31
+    return ((double)high * 4398046511104.0 + (double)(low & ((1ull << 42) - 1))) * (1.0 / 9007199254740992.0);
 }
 // Warp-wide (value desc, id asc) arg-max. Lanes without a candidate pass has = false. Returns the
 // winning id to every lane and its key through *key_out. At least one lane must have a candidate.

@@ -216,8 +216,7 @@ __global__ void __launch_bounds__(kThreads, 2) decode_small_gateup_kernel(Decode
         if (!GIVEN && (U > p.M || p.pool_ids != nullptr)) {
             // pool = best M experts of the union by (score desc, id asc): rank by counting over the members
             if (is_member) {
-                const unsigned long long acc = pool_sum(&sc.acc32[3 * tid]);
-                sc.key[mine] = score_order_key((double)acc * (1.0 / 9007199254740992.0) * (double)h_e);
+                sc.key[mine] = score_order_key(pool_sum(&sc.acc32[3 * tid]) * (double)h_e);
             }
             __syncthreads();
             int lanes = 32;  // threads per member

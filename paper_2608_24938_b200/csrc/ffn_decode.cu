@@ -339,9 +339,7 @@ __global__ void __launch_bounds__(kFThreads, 1) decode_ffn_kernel(const __grid_c
             const unsigned m = __ballot_sync(0xffffffffu, in);
             if (in && c % (kFThreads / 32) == warp) {
                 const int pos = U + __popc(m & ((1u << lane) - 1u));
-                const unsigned long long acc = pool_sum(&sc.acc32[3 * e]);
-                const long long key =
-                    score_order_key((double)acc * (1.0 / 9007199254740992.0) * (double)(c < kFThreads / 32 ? h_e[0] : h_e[1]));
+                const long long key = score_order_key(pool_sum(&sc.acc32[3 * e]) * (double)(c < kFThreads / 32 ? h_e[0] : h_e[1]));
                 member[pos] = e;
                 sc.key[pos] = key;
                 khi[pos] = (int)(key >> 32);

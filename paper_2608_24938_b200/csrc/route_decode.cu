@@ -28,7 +28,7 @@ struct DecSmem {
     float wrm[kDecMaxSlots];  // remapped weights
     long long key[kMaxExperts];           // order-preserving image of the expert's score
     unsigned long long acc[kMaxExperts];  // sum_i w_{i,e} in fixed point (2^-53 units): exact, order-independent
-    int in_union[kMaxExperts];            // 0, 1; given routes: 3 where the sum wrapped
+    int in_union[kMaxExperts];            // != 0: some token's; given routes: bit 0, and twice how often acc wrapped
     int rank_of[kMaxExperts];   // pool rank or -1
     int pool[kMaxExperts];      // pool ids by rank
     int target[kMaxExperts];
@@ -159,8 +159,12 @@ __global__ void __launch_bounds__(kDecThreads) decode_route_kernel(DecodeRoutePa
                     peer[r]->ids[i * K + lane] = my_id;
                     peer[r]->w64[i * K + lane] = wv;
                     const unsigned long long before = atomicAdd(&peer[r]->acc[my_id], fx);
-                    if constexpr (GIVEN) atomicOr(&peer[r]->in_union[my_id], before + fx < before ? 3 : 1);
-                    else peer[r]->in_union[my_id] = 1;
+                    if constexpr (GIVEN) {
+                        atomicOr(&peer[r]->in_union[my_id], 1);
+                        if (before + fx < before) atomicAdd(&peer[r]->in_union[my_id], 2);
+                    } else {
+                        peer[r]->in_union[my_id] = 1;
+                    }
                 }
         }
     }
@@ -186,8 +190,11 @@ __global__ void __launch_bounds__(kDecThreads) decode_route_kernel(DecodeRoutePa
     }
     // ---- Eq. 11: score_e = h_e * sum_i w_{i,e} (every CTA computes the same pool from the same sums)
     if (!is_static)
-        for (int e = threadIdx.x; e < N; e += kDecThreads)
-            sm.key[e] = score_order_key((double)(GIVEN && sm.in_union[e] > 1 ? ~0ull : sm.acc[e]) * (1.0 / 9007199254740992.0) * (double)sm.hh[e]);
+        for (int e = threadIdx.x; e < N; e += kDecThreads) {
+            double sum = (double)sm.acc[e] * (1.0 / 9007199254740992.0);
+            if (GIVEN) sum += 2048.0 * (double)(sm.in_union[e] >> 1);
+            sm.key[e] = score_order_key(sum * (double)sm.hh[e]);
+        }
     __syncthreads();
     // pool = best min(M, |U|) experts of the union by (score desc, id asc): rank by counting. Experts are
     // dealt round-robin over the CTAs, one warp per expert; ranks are broadcast to every copy.

@@ -378,3 +378,20 @@ def test_every_route_names_one_expert(ex, name, T):
     y, m = run_decode(case, case.xd, ids[:B], w[:B], cfg.n_experts)
     assert m["pool_size"][0] == 1 and m["pool_ids"][0] == 3
     check_output(y, experts(case, case.xd, one[:B], total[:B]), cfg.dtype)
+
+
+@pytest.mark.parametrize("name", ["tiny", "f32_shared", "bf16", "bf16_shared"])
+@pytest.mark.parametrize("scale", [16.0, 300.0, 1100.0])
+def test_decode_routed_ranks_large_sums(ex, name, scale):
+    """Sums of weights beyond 2048 rank as any others."""
+    cfg = CONFIGS[name]
+    for B in (8, 128, 256):
+        case = Case(dataclasses.replace(cfg, calib_tokens=0), B=B)
+        S, L, h, _ = case.np_tables()
+        ids, w = routes(cfg, B, seed=9)
+        w *= np.float32(scale)
+        for M in (1, cfg.n_experts // 2, cfg.n_experts):
+            pool, target, scale_, ri, rw = pool64(ids, w, M, S, L, h)
+            y, m = run_decode(case, case.xd, ids, w, M)
+            assert m["pool_ids"][:len(pool)].tolist() == pool and np.array_equal(m["ids"], ri)
+            check_output(y, experts(case, case.xd, ri, rw), cfg.dtype)
